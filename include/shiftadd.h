@@ -67,6 +67,9 @@ typedef enum {
 #define SA_MAX_BATCH 256
 #define SA_MAX_CYCLES 64
 #define SA_MAX_TERMS 4
+#define SA_MAX_ROWS (1 << 20)
+#define SA_MAX_EXPERTS 1024
+#define SA_MAX_CHOICES 16
 
 /* Bytes of the packed planes of a q x N x K layer: q*N*K/8 (1 bit per weight
  * per plane, no padding).  Returns 0 for invalid sizes. */
@@ -311,6 +314,116 @@ SA_API int sa_shiftadd_gemm_terms(const uint16_t *x, const uint8_t *packed_bits,
 
 /* Launch geometry of sa_shiftadd_gemm_blockwise (host-only). */
 SA_API int sa_plan_gemm_blockwise(int q, int N, int K, int row_block, int batch, sa_plan *plan);
+
+/* ---- The layer inside a model: what follows the product, and experts ----
+ *
+ * These calls take any number of rows (a token step, a prompt): 0 <= rows <=
+ * SA_MAX_ROWS and rows * N <= 2^34; with 0 rows they enqueue nothing and read
+ * no pointer.  All products are sums in fp32 and everything after them is fp32
+ * too; y is rounded once, as it is stored.  Deterministic; nothing is
+ * allocated; may be captured in a HIP graph. */
+
+typedef enum {
+    SA_ACT_NONE = 0,
+    SA_ACT_RELU = 1,      /* max(v, 0); a NaN stays one */
+    SA_ACT_GELU = 2,      /* v Phi(v) = v erfc(-v / sqrt 2) / 2 */
+    SA_ACT_GELU_TANH = 3, /* v (1 + tanh(sqrt(2 / pi) (v + 0.044715 v^3))) / 2 */
+    SA_ACT_SILU = 4       /* v / (1 + exp(-v)) */
+} sa_activation;
+
+/* The layer (row-wise factors, as sa_shiftadd_gemm) with what a model applies to
+ * its outputs:
+ *
+ *   y[r][n] = act(sum_k W_q[n][k] x[r][k] + bias[n]) * multiplier[r][n] + residual[r][n]
+ *
+ *   x, packed_bits, exps, q, N, K, group: as for sa_shiftadd_gemm, with `rows`
+ *               rows of x.
+ *   bias        (device) fp32 [N], 4-byte aligned, or NULL: none.
+ *   activation  sa_activation (else SA_ERR_SHAPE).
+ *   multiplier, residual  (device) [rows][N] of y's type, 16-byte aligned, or
+ *               NULL: none.  Either may be y itself (in place); other overlaps
+ *               of y with an input are not allowed.
+ *   out_half    1: y, multiplier and residual are binary16; 0: fp32.
+ *   y           (device) [rows][N], 16-byte aligned, fully overwritten.
+ * An infinity or NaN in a row of x makes that row's sums infinite or NaN and
+ * reaches no other row.  The sums are those of sa_shiftadd_gemm up to the order
+ * of their fp32 additions.  Errors as for sa_shiftadd_gemm. */
+SA_API int sa_shiftadd_gemm_epilogue(const uint16_t *x, const uint8_t *packed_bits,
+                                     const int8_t *exps, int q, int N, int K, int group, int rows,
+                                     const float *bias, int activation, const void *multiplier,
+                                     const void *residual, int out_half, void *y, void *stream);
+
+/* The same product for `experts` layers of one shape, each on its own rows (a
+ * mixture of experts): slot s in [offsets[e], offsets[e + 1]) belongs to expert e,
+ *
+ *   y[s][n] = act(sum_k W_q^e[n][k] x[row_of[s]][k] + bias[e][n]) * multiplier[s][n]
+ *
+ *   x           (device) binary16 [x_rows][K], 16-byte aligned.
+ *   row_of      (device) int32 [slots]: the row of x of each slot, or NULL: slot s
+ *               takes row s (then x_rows >= slots, else SA_ERR_SHAPE).
+ *   offsets     (device) int32 [experts + 1], ascending, within [0, slots].
+ *   packed_bits (device) experts x sa_packed_bytes(q, N, K) bytes, one layer after
+ *               the other; the first 16-byte aligned.
+ *   exps        (device) int8 [experts][q][N][K/group].
+ *   bias        (device) fp32 [experts][N] or NULL; multiplier (device) [slots][N]
+ *               of y's type or NULL, may be y itself.
+ *   y           (device) [slots][N], 16-byte aligned.
+ *   1 <= experts <= SA_MAX_EXPERTS; 0 <= slots <= SA_MAX_ROWS; 0 <= x_rows <=
+ *   SA_MAX_ROWS; slots * N <= 2^34 (else SA_ERR_SHAPE).
+ * Rows of y that belong to no expert (before offsets[0], from offsets[experts] on)
+ * and slots whose row_of lies outside [0, x_rows) are left as they were.
+ * Offsets are read on the device, so the split may come from a kernel enqueued
+ * before (sa_route_experts); values outside [0, slots] count as the nearest bound.
+ * Errors as for sa_shiftadd_gemm_epilogue. */
+SA_API int sa_shiftadd_gemm_experts(const uint16_t *x, int x_rows, const int32_t *row_of,
+                                    const int32_t *offsets, const uint8_t *packed_bits,
+                                    const int8_t *exps, int q, int N, int K, int group,
+                                    int experts, int slots, const float *bias, int activation,
+                                    const void *multiplier, int out_half, void *y, void *stream);
+
+/* A router's choice: each token's k experts of largest logit with their softmax
+ * weights, and the lists that sort the choices by expert.
+ *
+ *   ids[t][j]      the expert of the j-th largest logit of token t; equal logits by
+ *                  ascending number.  A logit of -inf (or NaN) is never chosen: where
+ *                  fewer than k are left, ids = -1, weights = 0, slot_of = -1.
+ *   weights[t][j]  exp(logit - m) / sum, m the token's largest logit, the sum over
+ *                  its choices (normalize = 1) or over all its experts (0).  A logit
+ *                  of +inf makes the token's weights NaN.
+ *   offsets[e]     the choices of experts below e; offsets[experts] all choices.
+ *   slot_of[t][j]  the place of choice (t, j) in the order by (expert, token).
+ *   row_of[s]      the token of slot s, -1 from offsets[experts] on.
+ *
+ *   logits (device) fp32 [tokens][experts]; ids, slot_of (device) int32 and weights
+ *   fp32 [tokens][k]; row_of int32 [tokens * k]; offsets int32 [experts + 1]; all
+ *   4-byte aligned and fully overwritten (tokens = 0: offsets alone, zeroed).
+ *   1 <= experts <= SA_MAX_EXPERTS; 1 <= k <= min(experts, SA_MAX_CHOICES);
+ *   0 <= tokens <= SA_MAX_ROWS (else SA_ERR_SHAPE).
+ *   workspace (device) >= sa_route_workspace_bytes(tokens, experts, k) bytes, 16-byte
+ *   aligned, owned by the caller, overwritten; calls that share one must not
+ *   overlap (nor graphs that captured it); NULL where that size is 0.
+ * Deterministic.  Asynchronous on `stream`; allocates nothing. */
+SA_API size_t sa_route_workspace_bytes(int tokens, int experts, int k);
+SA_API int sa_route_experts(const float *logits, int tokens, int experts, int k, int normalize,
+                            int32_t *ids, float *weights, int32_t *offsets, int32_t *row_of,
+                            int32_t *slot_of, void *workspace, size_t workspace_bytes,
+                            void *stream);
+
+/* The sum of each token's expert rows:
+ *
+ *   y[t][n] = residual[t][n] + sum_j weights[t][j] h[slot_of[t][j]][n]
+ *
+ * in fp32, j ascending, rounded once; a slot_of outside [0, slots) adds nothing,
+ * whatever its weight.
+ *   h (device) [slots][N]; residual (device) [tokens][N] or NULL (0), may be y
+ *   itself; y (device) [tokens][N], fully overwritten: binary16 (half = 1) or fp32
+ *   (0), each 16-byte aligned.  slot_of (device) int32, weights (device) fp32
+ *   [tokens][k], 4-byte aligned.
+ *   1 <= k <= SA_MAX_CHOICES; N >= 1; 0 <= slots, tokens <= SA_MAX_ROWS; tokens * N
+ *   and slots * N <= 2^34 (else SA_ERR_SHAPE).  Asynchronous on `stream`. */
+SA_API int sa_combine_experts(const void *h, const int32_t *slot_of, const float *weights,
+                              int slots, int tokens, int k, int N, const void *residual, int half,
+                              void *y, void *stream);
 
 /* ---- Automated mixed-bit allocation (Sec. 4.3, Eq. 3 and Eq. 4) ----
  *

@@ -16,6 +16,8 @@ __all__ = [
     "sa_importance_criterion", "sa_fit_per_bit", "sa_allocate_bits", "bit_criterion",
     "pack_weights", "shiftadd_gemm", "SaError", "sa_shiftadd_gemm_kslice",
     "sa_kslice_workspace_bytes", "sa_shiftadd_gemm_f16",
+    "sa_shiftadd_gemm_epilogue", "sa_shiftadd_gemm_experts", "sa_route_workspace_bytes",
+    "sa_route_experts", "sa_combine_experts", "shiftadd_linear", "route_experts", "shiftadd_moe",
 ]
 
 

@@ -8,6 +8,21 @@
 
 __host__ __device__ inline int imin(int a, int b) { return a < b ? a : b; }
 
+// Byte offset of the key of (plane i, row n, chunk c) in the packed layout.
+// Rows come in tiles of 64 and chunks in blocks of 16; a 64-row tile of one
+// block is a contiguous piece, 16 bytes per row.  Inside a full block the 16
+// keys of row r are rotated by r: position p holds chunk (p + r) mod 16, so
+// that the lanes of a wave querying position p touch 16 different tables.
+__host__ __device__ inline int64_t layout_offset(int i, int n, int c, int N, int C) {
+    const int T = n >> 6, r = n & 63;
+    const int R = imin(64, N - 64 * T);
+    const int J = c >> 4, u = c & 15;
+    const int U = imin(16, C - 16 * J);
+    const int p = (U == 16) ? ((u - r) & 15) : u;
+    return ((int64_t)i * N + (int64_t)64 * T) * C + (int64_t)16 * J * R +
+           (int64_t)r * U + p;
+}
+
 // Bytes of v rotated so that byte p of the result is byte (p + r) mod 16 of v.  The
 // key at position p of a row is chunk (p + row) mod 16 of its block: rotating 16
 // exponents in chunk order by the row lines them up with the keys, rotating the

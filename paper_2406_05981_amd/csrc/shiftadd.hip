@@ -10,6 +10,7 @@
 
 #include <stdint.h>
 
+#include "checks.h"
 #include "gemm_matrix.h"
 #include "keys.h"
 #include "shiftadd.h"
@@ -22,21 +23,6 @@ constexpr int kThreads = 256;     // 4 waves of 64
 constexpr int kTileRows = 64;     // rows per tile: one row per lane
 constexpr int kBlockChunks = 16;  // chunks (8 columns each) per block: 128 columns
 constexpr int kKeyStride = 64;    // floats per key in the LDS tables (256 bytes)
-
-// Byte offset of the key of (plane i, row n, chunk c) in the packed layout.
-// Rows come in tiles of 64 and chunks in blocks of 16; a 64-row tile of one
-// block is a contiguous piece, 16 bytes per row.  Inside a full block the 16
-// keys of row r are rotated by r: position p holds chunk (p + r) mod 16, so
-// that the lanes of a wave querying position p touch 16 different tables.
-__host__ __device__ inline int64_t layout_offset(int i, int n, int c, int N, int C) {
-    const int T = n >> 6, r = n & 63;
-    const int R = imin(kTileRows, N - kTileRows * T);
-    const int J = c >> 4, u = c & 15;
-    const int U = imin(kBlockChunks, C - kBlockChunks * J);
-    const int p = (U == kBlockChunks) ? ((u - r) & 15) : u;
-    return ((int64_t)i * N + (int64_t)kTileRows * T) * C + (int64_t)kBlockChunks * J * R +
-           (int64_t)r * U + p;
-}
 
 // One output: fp32, or IEEE binary16 rounded to nearest even when `half` (the
 // fp16 output activations of Sec. 4.1; y then holds binary16 bit patterns).
@@ -1406,18 +1392,6 @@ __global__ __launch_bounds__(kProbeThreads) void k_read_probe(const uint4* __res
 
 // ---------------------------------------------------------------- host side
 
-bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
-
-int check_dims(int q, int N, int K) {
-    if (q < 1 || q > SA_MAX_Q) return SA_ERR_Q;
-    if (N < 1 || K < 8 || (K & 7)) return SA_ERR_SHAPE;
-    // every element count that the kernels index must fit comfortably; one
-    // plane of packed keys stays below 2^31 bytes (32-bit per-lane offsets)
-    if ((int64_t)q * N * K > (int64_t)1 << 36) return SA_ERR_SHAPE;
-    if ((int64_t)N * (K / 8) >= (int64_t)1 << 31) return SA_ERR_SHAPE;
-    return SA_OK;
-}
-
 int validate_gemm(const void* x, const void* packed, const void* exps, int q, int N, int K,
                   int group, int batch, const void* y) {
     if (!x || !packed || !exps || !y) return SA_ERR_NULL;
@@ -1587,8 +1561,6 @@ void make_matrix_plan(int q, int N, int K, int group, int terms, int batch, sa_m
     us = sa_mfma::plan(q, N, K, group, batch, terms, &c);
     if (us < best) *p = c;
 }
-
-int launch_status() { return hipGetLastError() == hipSuccess ? SA_OK : SA_ERR_HIP; }
 
 int grid_for(int64_t items) {
     int64_t g = (items + kThreads - 1) / kThreads;

@@ -62,6 +62,12 @@ def _bind(lib):
         "sa_shiftadd_gemm_blockwise": ([P, P, P, I, I, I, I, I, P, P], I),
         "sa_plan_gemm_blockwise": ([I, I, I, I, I, ctypes.POINTER(SaPlan)], I),
         "sa_shiftadd_gemm_terms": ([P, P, P, P, I, I, I, I, I, I, P, P], I),
+        "sa_shiftadd_gemm_epilogue": ([P, P, P, I, I, I, I, I, P, I, P, P, I, P, P], I),
+        "sa_shiftadd_gemm_experts": (
+            [P, I, P, P, P, P, I, I, I, I, I, I, P, I, P, I, P, P], I),
+        "sa_route_workspace_bytes": ([I, I, I], ctypes.c_size_t),
+        "sa_route_experts": ([P, I, I, I, I, P, P, P, P, P, P, ctypes.c_size_t, P], I),
+        "sa_combine_experts": ([P, P, P, I, I, I, I, P, I, P, P], I),
         "sa_read_probe": ([P, ctypes.c_size_t, P, P], I),
         "sa_quantize_bcq": ([P, I, I, I, I, I, P, P, P], I),
         "sa_quantize_bcq_terms": ([P, I, I, I, I, I, I, P, P, P, P], I),
@@ -91,6 +97,12 @@ SA_MAX_Q = 8
 SA_MAX_BATCH = 256
 SA_MAX_CYCLES = 64
 SA_MAX_TERMS = 4
+SA_MAX_ROWS = 1 << 20
+SA_MAX_EXPERTS = 1024
+SA_MAX_CHOICES = 16
+
+# sa_activation
+ACTIVATIONS = {"none": 0, "relu": 1, "gelu": 2, "gelu_tanh": 3, "silu": 4}
 
 
 class SaError(RuntimeError):
@@ -133,6 +145,24 @@ def _dev(t: torch.Tensor, name: str, dtype: torch.dtype, numel: int) -> int:
     if t.numel() != numel:
         raise ValueError(f"{name} must have {numel} elements, got {t.numel()}")
     return t.data_ptr()
+
+
+def _opt(t: Optional[torch.Tensor], name: str, dtype: torch.dtype, numel: int) -> Optional[int]:
+    return None if t is None else _dev(t, name, dtype, numel)
+
+
+def _activation(name: str) -> int:
+    if name not in ACTIVATIONS:
+        raise ValueError(f"activation must be one of {', '.join(ACTIVATIONS)}, got {name!r}")
+    return ACTIVATIONS[name]
+
+
+def _out_half(y: torch.Tensor) -> int:
+    if not isinstance(y, torch.Tensor):
+        raise TypeError("y must be a torch.Tensor")
+    if y.dtype not in (torch.float16, torch.float32):
+        raise ValueError(f"y must be torch.float16 or torch.float32, got {y.dtype}")
+    return int(y.dtype == torch.float16)
 
 
 def sa_status_string(status: int) -> str:
@@ -295,6 +325,91 @@ def sa_shiftadd_gemm_terms(x: torch.Tensor, packed_bits: torch.Tensor, exps: tor
         _dev(y, "y", torch.float32, batch * N), _stream(stream)), "sa_shiftadd_gemm_terms")
 
 
+def sa_shiftadd_gemm_epilogue(x: torch.Tensor, packed_bits: torch.Tensor, exps: torch.Tensor,
+                              q: int, N: int, K: int, group: int, rows: int,
+                              bias: Optional[torch.Tensor], activation: str,
+                              multiplier: Optional[torch.Tensor],
+                              residual: Optional[torch.Tensor], y: torch.Tensor,
+                              stream=None) -> None:
+    """``y = activation(x W_q^T + bias) * multiplier + residual``; fp32 or binary16 by
+    ``y``'s type, which ``multiplier`` and ``residual`` share."""
+    if sa_packed_bytes(q, N, K) == 0:
+        _check(SA_ERR_SHAPE if 1 <= q <= SA_MAX_Q else SA_ERR_Q, "sa_shiftadd_gemm_epilogue")
+    if group <= 0 or K % group:
+        _check(SA_ERR_GROUP, "sa_shiftadd_gemm_epilogue")
+    half = _out_half(y)
+    _check(lib.sa_shiftadd_gemm_epilogue(
+        _dev(x, "x", torch.float16, rows * K),
+        _dev(packed_bits, "packed_bits", torch.uint8, sa_packed_bytes(q, N, K)),
+        _dev(exps, "exps", torch.int8, q * N * (K // group)),
+        q, N, K, group, rows, _opt(bias, "bias", torch.float32, N), _activation(activation),
+        _opt(multiplier, "multiplier", y.dtype, rows * N),
+        _opt(residual, "residual", y.dtype, rows * N),
+        half, _dev(y, "y", y.dtype, rows * N), _stream(stream)), "sa_shiftadd_gemm_epilogue")
+
+
+def sa_shiftadd_gemm_experts(x: torch.Tensor, row_of: Optional[torch.Tensor],
+                             offsets: torch.Tensor, packed_bits: torch.Tensor,
+                             exps: torch.Tensor, q: int, N: int, K: int, group: int,
+                             experts: int, slots: int, bias: Optional[torch.Tensor],
+                             activation: str, multiplier: Optional[torch.Tensor],
+                             y: torch.Tensor, stream=None) -> None:
+    """``y[s] = activation(x[row_of[s]] W_q^e^T + bias[e]) * multiplier[s]`` for the slots
+    ``offsets[e] <= s < offsets[e + 1]`` of every expert e."""
+    if sa_packed_bytes(q, N, K) == 0:
+        _check(SA_ERR_SHAPE if 1 <= q <= SA_MAX_Q else SA_ERR_Q, "sa_shiftadd_gemm_experts")
+    if group <= 0 or K % group:
+        _check(SA_ERR_GROUP, "sa_shiftadd_gemm_experts")
+    half = _out_half(y)
+    x_rows = x.numel() // K if isinstance(x, torch.Tensor) else 0
+    _check(lib.sa_shiftadd_gemm_experts(
+        _dev(x, "x", torch.float16, x_rows * K), x_rows,
+        _opt(row_of, "row_of", torch.int32, slots),
+        _dev(offsets, "offsets", torch.int32, experts + 1),
+        _dev(packed_bits, "packed_bits", torch.uint8, experts * sa_packed_bytes(q, N, K)),
+        _dev(exps, "exps", torch.int8, experts * q * N * (K // group)),
+        q, N, K, group, experts, slots, _opt(bias, "bias", torch.float32, experts * N),
+        _activation(activation), _opt(multiplier, "multiplier", y.dtype, slots * N),
+        half, _dev(y, "y", y.dtype, slots * N), _stream(stream)), "sa_shiftadd_gemm_experts")
+
+
+def sa_route_workspace_bytes(tokens: int, experts: int, k: int) -> int:
+    return int(lib.sa_route_workspace_bytes(tokens, experts, k))
+
+
+def sa_route_experts(logits: torch.Tensor, tokens: int, experts: int, k: int, normalize: bool,
+                     ids: torch.Tensor, weights: torch.Tensor, offsets: torch.Tensor,
+                     row_of: torch.Tensor, slot_of: torch.Tensor,
+                     workspace: Optional[torch.Tensor] = None, stream=None) -> None:
+    nbytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    _check(lib.sa_route_experts(
+        _dev(logits, "logits", torch.float32, tokens * experts), tokens, experts, k,
+        int(bool(normalize)), _dev(ids, "ids", torch.int32, tokens * k),
+        _dev(weights, "weights", torch.float32, tokens * k),
+        _dev(offsets, "offsets", torch.int32, experts + 1),
+        _dev(row_of, "row_of", torch.int32, tokens * k),
+        _dev(slot_of, "slot_of", torch.int32, tokens * k),
+        None if workspace is None else _dev(workspace, "workspace", workspace.dtype,
+                                            workspace.numel()),
+        nbytes, _stream(stream)), "sa_route_experts")
+
+
+def sa_combine_experts(h: torch.Tensor, slot_of: torch.Tensor, weights: torch.Tensor, tokens: int,
+                       k: int, N: int, residual: Optional[torch.Tensor], y: torch.Tensor,
+                       stream=None) -> None:
+    """``y[t] = residual[t] + sum_j weights[t][j] h[slot_of[t][j]]``; ``h``, ``residual`` and
+    ``y`` of one type, fp32 or binary16."""
+    half = _out_half(y)
+    if N < 1:
+        _check(SA_ERR_SHAPE, "sa_combine_experts")
+    slots = h.numel() // N if isinstance(h, torch.Tensor) else 0
+    _check(lib.sa_combine_experts(
+        _dev(h, "h", y.dtype, slots * N), _dev(slot_of, "slot_of", torch.int32, tokens * k),
+        _dev(weights, "weights", torch.float32, tokens * k), slots, tokens, k, N,
+        _opt(residual, "residual", y.dtype, tokens * N), half,
+        _dev(y, "y", y.dtype, tokens * N), _stream(stream)), "sa_combine_experts")
+
+
 def sa_quantize_bcq(w: torch.Tensor, N: int, K: int, q: int, group: int, cycles: int,
                     signs: torch.Tensor, exps: torch.Tensor, stream=None) -> None:
     if group <= 0 or K % group:
@@ -453,6 +568,58 @@ def shiftadd_gemm_blockwise(x: torch.Tensor, packed_bits: torch.Tensor, blk_exps
     batch = x.shape[0] if x.dim() == 2 else 1
     y = out if out is not None else torch.empty((batch, N), dtype=torch.float32, device=x.device)
     sa_shiftadd_gemm_blockwise(x, packed_bits, blk_exps, q, N, K, row_block, batch, y, stream)
+    return y
+
+
+def shiftadd_linear(x: torch.Tensor, packed_bits: torch.Tensor, exps: torch.Tensor, q: int, N: int,
+                    K: int, group: int, bias: Optional[torch.Tensor] = None,
+                    activation: str = "none", multiplier: Optional[torch.Tensor] = None,
+                    residual: Optional[torch.Tensor] = None,
+                    out_dtype: torch.dtype = torch.float16, out: Optional[torch.Tensor] = None,
+                    stream=None) -> torch.Tensor:
+    """``activation(x W_q^T + bias) * multiplier + residual`` of any number of rows as a new
+    (or the given) ``[rows][N]`` tensor."""
+    rows = x.numel() // K
+    y = out if out is not None else torch.empty((rows, N), dtype=out_dtype, device=x.device)
+    sa_shiftadd_gemm_epilogue(x, packed_bits, exps, q, N, K, group, rows, bias, activation,
+                              multiplier, residual, y, stream)
+    return y
+
+
+def route_experts(logits: torch.Tensor, k: int, normalize: bool = True, stream=None):
+    """``(ids, weights, offsets, row_of, slot_of)`` of fp32 router logits
+    ``[tokens][experts]`` (new device tensors)."""
+    tokens, experts = logits.shape
+    new = lambda *shape: torch.empty(shape, dtype=torch.int32, device=logits.device)  # noqa: E731
+    ids, slot_of, row_of, offsets = new(tokens, k), new(tokens, k), new(tokens * k), new(experts + 1)
+    weights = torch.empty((tokens, k), dtype=torch.float32, device=logits.device)
+    workspace = torch.empty(sa_route_workspace_bytes(tokens, experts, k), dtype=torch.uint8,
+                            device=logits.device)
+    sa_route_experts(logits, tokens, experts, k, normalize, ids, weights, offsets, row_of, slot_of,
+                     workspace, stream)
+    return ids, weights, offsets, row_of, slot_of
+
+
+def shiftadd_moe(x: torch.Tensor, logits: torch.Tensor, k: int, gate, up, down, N: int, K: int,
+                 group: int, residual: Optional[torch.Tensor] = None, normalize: bool = True,
+                 stream=None) -> torch.Tensor:
+    """A gated mixture-of-experts block, ``residual + sum_j w_j D_e(silu(G_e x) * U_e x)`` over
+    each token's ``k`` experts, as a new fp16 ``[tokens][K]`` tensor.  ``gate``, ``up`` (N x K
+    layers) and ``down`` (K x N) are ``(packed_bits, exps, q)`` of all experts; ``logits`` fp32
+    ``[tokens][experts]``."""
+    tokens, experts = logits.shape
+    slots = tokens * k
+    _, weights, offsets, row_of, slot_of = route_experts(logits, k, normalize, stream)
+    new = lambda n: torch.empty((slots, n), dtype=torch.float16, device=x.device)  # noqa: E731
+    h, out = new(N), new(K)
+    sa_shiftadd_gemm_experts(x, row_of, offsets, up[0], up[1], up[2], N, K, group, experts, slots,
+                             None, "none", None, h, stream)
+    sa_shiftadd_gemm_experts(x, row_of, offsets, gate[0], gate[1], gate[2], N, K, group, experts,
+                             slots, None, "silu", h, h, stream)
+    sa_shiftadd_gemm_experts(h, None, offsets, down[0], down[1], down[2], K, N, group, experts,
+                             slots, None, "none", None, out, stream)
+    y = torch.empty((tokens, K), dtype=torch.float16, device=x.device)
+    sa_combine_experts(out, slot_of, weights, tokens, k, K, residual, y, stream)
     return y
 
 
