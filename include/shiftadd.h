@@ -318,8 +318,9 @@ SA_API int sa_plan_gemm_blockwise(int q, int N, int K, int row_block, int batch,
 /* ---- The layer inside a model: what follows the product, and experts ----
  *
  * These calls take any number of rows (a token step, a prompt): 0 <= rows <=
- * SA_MAX_ROWS and rows * N <= 2^34; with 0 rows they enqueue nothing and read
- * no pointer.  All products are sums in fp32 and everything after them is fp32
+ * SA_MAX_ROWS, rows * K <= 2^35 and (ceil(rows / 32) + experts) * ceil(N / 32) <
+ * 2^23 (8.5e9 outputs), else SA_ERR_SHAPE; with 0 rows they enqueue nothing and
+ * read no pointer.  All products are sums in fp32 and everything after them is fp32
  * too; y is rounded once, as it is stored.  Deterministic; nothing is
  * allocated; may be captured in a HIP graph. */
 
@@ -368,8 +369,8 @@ SA_API int sa_shiftadd_gemm_epilogue(const uint16_t *x, const uint8_t *packed_bi
  *   bias        (device) fp32 [experts][N] or NULL; multiplier (device) [slots][N]
  *               of y's type or NULL, may be y itself.
  *   y           (device) [slots][N], 16-byte aligned.
- *   1 <= experts <= SA_MAX_EXPERTS; 0 <= slots <= SA_MAX_ROWS; 0 <= x_rows <=
- *   SA_MAX_ROWS; slots * N <= 2^34 (else SA_ERR_SHAPE).
+ *   1 <= experts <= SA_MAX_EXPERTS; slots (0 allowed) as the rows above and x_rows
+ *   in [0, SA_MAX_ROWS] with x_rows * K <= 2^35 (else SA_ERR_SHAPE).
  * Rows of y that belong to no expert (before offsets[0], from offsets[experts] on)
  * and slots whose row_of lies outside [0, x_rows) are left as they were.
  * Offsets are read on the device, so the split may come from a kernel enqueued

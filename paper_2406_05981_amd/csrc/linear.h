@@ -1,0 +1,88 @@
+// The layer with its epilogue, on one layer or on experts with ragged rows: what the
+// kernels of linear.hip and panel.hip share.
+#ifndef SHIFTADD_LINEAR_H
+#define SHIFTADD_LINEAR_H
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "epilogue.h"
+#include "keys.h"
+
+namespace sa_linear {
+
+struct Layer {
+    const uint16_t* x;       // activations [x_rows][K]
+    const uint8_t* packed;   // planes of the first layer
+    const int8_t* exps;      // [q][N][K/G] of the first layer
+    const int32_t* row_of;   // row of x of each row of y, or null: the row itself
+    const int32_t* offsets;  // experts: rows of y of each; null: one layer, all rows
+    int q, N, K, G;
+    int rows;     // rows of y
+    int x_rows;   // rows of x
+    int experts;  // layers
+    sa_epi::Epilogue epi;
+};
+
+// The `tile`-th tile of `height` rows, counted over the experts' rows: its expert and
+// rows [first, end).  Every lane of a wave calls it; false past the last tile.
+__device__ inline bool find_tile(const Layer& a, int height, int tile, int* expert, int* first,
+                                 int* end) {
+    if (!a.offsets) {
+        *expert = 0;
+        *first = tile * height;
+        *end = a.rows;
+        return *first < a.rows;
+    }
+    const int lane = threadIdx.x & 63;
+    int before = 0;  // tiles of the experts below e0
+    for (int e0 = 0; e0 < a.experts; e0 += 64) {
+        const int e = e0 + lane;
+        int lo = 0, hi = 0;
+        if (e < a.experts) {
+            lo = imin(max(a.offsets[e], 0), a.rows);
+            hi = imin(max(a.offsets[e + 1], lo), a.rows);
+        }
+        const int tiles = (hi - lo + height - 1) / height;
+        int sum = tiles;
+#pragma unroll
+        for (int d = 1; d < 64; d <<= 1) {
+            const int v = __shfl_up(sum, d);
+            if (lane >= d) sum += v;
+        }
+        const int total = __shfl(sum, 63);
+        if (tile < before + total) {
+            const int l = __builtin_ctzll(__ballot(tile < before + sum));
+            const int f = __shfl(lo, l) + height * (tile - before - __shfl(sum - tiles, l));
+            *expert = __builtin_amdgcn_readfirstlane(e0 + l);
+            *first = __builtin_amdgcn_readfirstlane(f);
+            *end = __builtin_amdgcn_readfirstlane(__shfl(hi, l));
+            return true;
+        }
+        before += total;
+    }
+    return false;
+}
+
+// The row of x of row `row` of y, or -1: none.
+__device__ inline int source_row(const Layer& a, int row) {
+    if (!a.row_of) return row;
+    const int v = a.row_of[row];
+    return v >= 0 && v < a.x_rows ? v : -1;
+}
+
+// Tiles of `height` rows that any split of the rows over the experts can have.
+inline int64_t most_tiles(const Layer& a, int height) {
+    if (!a.offsets) return ((int64_t)a.rows + height - 1) / height;
+    const int64_t t = ((int64_t)a.rows + (int64_t)a.experts * (height - 1)) / height;
+    return t < a.rows ? t : a.rows;
+}
+
+}  // namespace sa_linear
+
+// Any rows, groups and planes.
+namespace sa_panel {
+void launch(const sa_linear::Layer& a, hipStream_t s);
+}  // namespace sa_panel
+
+#endif

@@ -1,0 +1,517 @@
+// The layer for many rows on the binary16 matrix cores, the planes summed first.
+//
+//   y[r][n] = act(sum_k W[n][k] x[r][k] + bias[n]) * multiplier[r][n] + residual[r][n]
+//
+// W[n][k] = sum_i +-2^e_i is one binary16 number wherever the exponents of a
+// (row, group) lie in [-14, 0] and q 2^(largest - smallest) <= 2^11: every partial
+// sum is a multiple of the smallest factor, at most 2^11 of it, so the sum over the
+// planes is exact and one matrix product serves all planes.  (Below -14 the sum may
+// be subnormal, and the matrix core then drops low bits of its products: measured
+// 7e-6 of sum|terms| at 2^-24.)  A block of 128 columns
+// that has any other exponents in a wave's rows takes two products a plane: +-2^e is a
+// bfloat16 number, an activation the sum of two.
+#include <hip/hip_runtime.h>
+
+#include <type_traits>
+
+#include "linear.h"
+
+namespace sa_panel {
+namespace {
+
+using sa_linear::Layer;
+
+typedef _Float16 half2_t __attribute__((ext_vector_type(2)));
+typedef _Float16 half8_t __attribute__((ext_vector_type(8)));
+typedef __bf16 bhalf8_t __attribute__((ext_vector_type(8)));
+typedef float float16_t __attribute__((ext_vector_type(16)));
+
+constexpr int kWaves = 8;
+constexpr int kThreads = 64 * kWaves;
+constexpr int kTile = 32;  // outputs and rows of one matrix tile
+
+struct Args {
+    Layer a;
+    int n_tiles;           // tiles of outputs; they run fastest over the grid
+    uint32_t group_magic;  // blocks to exponent groups: J * magic >> 32, 0: J
+    int vector_out;        // rows of y divide into vectors of 8
+};
+
+__device__ inline half2_t halves(uint32_t v) { return __builtin_bit_cast(half2_t, v); }
+__device__ inline half2_t both(float v) { return half2_t{(_Float16)v, (_Float16)v}; }
+
+__device__ inline half8_t cat(const half2_t a[4]) {
+    return half8_t{a[0][0], a[0][1], a[1][0], a[1][1], a[2][0], a[2][1], a[3][0], a[3][1]};
+}
+
+// A key byte is eight columns.  Half h of a key word (bytes 2 h, 2 h + 1) is spread so
+// that an even position p of either 16-bit half holds bits p and p + 1 of the two bytes;
+// a bit at position 10, 12 or 14 of a half is the binary16 value 2^-14, 2^-11 or 2, and
+// two shifted copies bring the other positions there.
+struct Spread {
+    uint32_t v, v6, v12;
+};
+__device__ inline Spread spread(uint32_t w, int h) {
+    const uint32_t v = __builtin_amdgcn_perm(w >> 1, w, h ? 0x07060302u : 0x05040100u);
+    return {v, v << 6, v << 12};
+}
+
+// A factor f = 2^e, -14 <= e <= 0, as what turns the bit values into 0 or 2 f: times
+// f 2^15, f 2^12 and f (normal numbers, built from e).
+struct Factor {
+    half2_t m10, m12, m14;
+};
+__device__ inline Factor factor(int e) {
+    const uint32_t h = (uint32_t)(e << 10) + (30u << 10);
+    const uint32_t m = h | h << 16;
+    return {halves(m), halves(m - 0x0C000C00u), halves(m - 0x3C003C00u)};
+}
+
+// Pair j of byte 2 h + odd: c += (bit ? 2 f : 0).
+__device__ inline half2_t add_pair(const Spread& s, const Factor& f, int odd, int j, half2_t c) {
+    const uint32_t src = odd ? (j == 0 ? s.v6 : s.v) : (j < 2 ? s.v12 : s.v6);
+    const int pos = odd ? (j == 0 ? 14 : 8 + 2 * j) : (j < 2 ? 12 + 2 * j : 6 + 2 * j);
+    const half2_t m = pos == 10 ? f.m10 : pos == 12 ? f.m12 : f.m14;
+    return __builtin_elementwise_fma(halves(src & (0x00010001u << pos)), m, c);
+}
+
+__device__ inline void copy_to_lds(const uint4* from, uint4* to) {
+    __builtin_amdgcn_global_load_lds(
+        (const __attribute__((address_space(1))) void*)(uintptr_t)from,
+        (__attribute__((address_space(3))) void*)to, 16, 0, 0);
+}
+
+__device__ inline void wave_fence() {
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
+// Keys and exponents as loaded.  Lane (i, g) has a layer row and, of a group of two
+// blocks, the 16 keys and the exponent of block g.  GEN: of one block, the keys of its
+// chunks g, 2 + g, ..., 14 + g in w.x, w.y and their exponents in w.z, w.w.
+template <int Q, bool GEN>
+struct Keys {
+    uint4 w[Q];
+    uint32_t e[GEN ? 1 : Q];
+};
+
+// Work split.  Eight waves are RW sets of 32 outputs times KW shares of the columns; a
+// wave has all 32 CT rows of the workgroup.  Activations of a 128-column block lie in
+// LDS, double buffered and copied there without passing registers; the planes are
+// expanded straight into matrix operands.  KW shares' sums meet in LDS and are added in
+// order.
+//
+// Matrix row i of a wave is output 16 ((i >> 2) & 1) + 4 (i >> 3) + (i & 3) of its 32, so
+// that a lane's 16 results are 16 consecutive outputs of one row.  Step s of a block
+// multiplies its chunks 2 s (lanes 0-31) and 2 s + 1 (lanes 32-63).  A row's 16 chunks of
+// a block are 256 bytes of LDS, chunk c at 16 (c ^ (row & 15)): both the copies (whole
+// rows) and the reads (16 lanes at a time, one step) touch every bank once.
+template <int Q, int CT, int KW, bool GEN>
+__device__ __forceinline__ void body(const Args& pa, uint4* xbuf) {
+    const Layer& a = pa.a;
+    constexpr int RW = kWaves / KW;
+    constexpr int kItems = CT * 8 / RW;  // 1 KiB copies (4 rows) of a wave a block
+    constexpr int kBuf = CT * 512;       // uint4 of one block
+    constexpr int kE = Q > 4 ? 2 : 1;    // words of a block's exponents
+    int expert, first, end;
+    if (!sa_linear::find_tile(a, kTile * CT, (int)(blockIdx.x / (unsigned)pa.n_tiles), &expert,
+                              &first, &end))
+        return;
+    const int nt = (int)(blockIdx.x % (unsigned)pa.n_tiles);
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    const int r = lane & 31, g = lane >> 5;
+    const int rw = wave % RW, kw = wave / RW;
+    const int N = a.N, C = a.K >> 3, NB = (C + 15) >> 4, NG = a.K / a.G;
+    const int gper = ((NB + 1) / 2 + KW - 1) / KW;  // groups of two blocks of a column share
+    const int blk0 = imin(2 * gper * kw, NB), blk1 = imin(blk0 + 2 * gper, NB);
+    const int steps = imin(2 * gper, NB);
+    const uint8_t* packed = a.packed + (int64_t)expert * a.q * N * C;
+    const uint8_t* exps =
+        reinterpret_cast<const uint8_t*>(a.exps) + (int64_t)expert * a.q * N * NG;
+    const int n0 = kTile * (RW * nt + rw);  // first output of this wave
+    const int n = imin(n0 + 16 * ((r >> 2) & 1) + 4 * (r >> 3) + (r & 3), N - 1);
+
+    // rows of x that this lane copies, as 16-byte words from a.x (x is below 2^36 bytes)
+    uint32_t xo[kItems];
+#pragma unroll
+    for (int j = 0; j < kItems; ++j) {
+        const int row = 4 * (rw * kItems + j) + (lane >> 4);
+        const int v = sa_linear::source_row(a, imin(first + row, end - 1));
+        xo[j] = (uint32_t)max(v, 0) * (uint32_t)C;
+        if constexpr (!GEN) xo[j] += (uint32_t)((lane & 15) ^ (row & 15));
+    }
+    uint4* xk = xbuf + kw * 2 * kBuf;
+    auto copy_x = [&](int J, int buf) {
+        const uint4* base = reinterpret_cast<const uint4*>(a.x) + (GEN ? 0 : 16 * (int64_t)J);
+#pragma unroll
+        for (int j = 0; j < kItems; ++j) {
+            uint32_t o = xo[j];
+            asm volatile("" : "+v"(o));  // (no 64-bit pointers kept over the blocks)
+            if constexpr (GEN) {
+                const int row = 4 * (rw * kItems + j) + (lane >> 4);
+                o += (uint32_t)imin(16 * J + ((lane & 15) ^ (row & 15)), C - 1);
+            }
+            copy_to_lds(base + o, xk + buf * kBuf + (rw * kItems + j) * 64);
+        }
+    };
+    // this lane's activations of step s, row tile c: word 512 c + ((2 s) ^ x_word)
+    const uint4* xr = xk + r * 16;
+    const int x_word = g ^ (r & 15);
+    // the copies of this wave are done, and every wave's
+    auto arrive = [] {
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        __syncthreads();
+    };
+
+    // Planes past the last repeat it, unused.
+    auto load_keys = [&](int J0, Keys<Q, GEN>& k) {
+        const uint32_t eoff = (uint32_t)n * (uint32_t)NG;
+        if constexpr (GEN) {
+            const int gc = a.G >> 3;
+#pragma unroll
+            for (int i = 0; i < Q; ++i) {
+                const int pi = imin(i, a.q - 1);
+                const uint8_t* ep = exps + (size_t)pi * (size_t)N * (size_t)NG;
+                uint32_t b[2] = {0, 0}, e[2] = {0, 0};
+#pragma unroll
+                for (int s = 0; s < 8; ++s) {
+                    const int c = imin(16 * J0 + 2 * s + g, C - 1);
+                    b[s >> 2] |= (uint32_t)packed[layout_offset(pi, n, c, N, C)] << (8 * (s & 3));
+                    e[s >> 2] |= (uint32_t)ep[eoff + (uint32_t)(c / gc)] << (8 * (s & 3));
+                }
+                k.w[i] = uint4{b[0], b[1], e[0], e[1]};
+            }
+        } else {
+            const int J = imin(J0 + g, NB - 1);
+            const uint32_t group =
+                pa.group_magic ? __umulhi((uint32_t)J, pa.group_magic) : (uint32_t)J;
+            const int T = n >> 6, R = imin(64, N - 64 * T);
+            uint32_t koff = (uint32_t)(64 * T * C + 16 * (n & 63) + 16 * J * R);
+            asm volatile("" : "+v"(koff));
+#pragma unroll
+            for (int i = 0; i < Q; ++i)
+                k.e[i] = (exps + (size_t)imin(i, a.q - 1) * (size_t)N * (size_t)NG)[eoff + group];
+#pragma unroll
+            for (int i = 0; i < Q; ++i)
+                k.w[i] = *reinterpret_cast<const uint4*>(
+                    packed + (size_t)imin(i, a.q - 1) * (size_t)N * (size_t)C + koff);
+        }
+    };
+
+    float16_t acc[CT];
+#pragma unroll
+    for (int c = 0; c < CT; ++c)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) acc[c][v] = 0.0f;
+
+    // GEN: columns past the last hold no weight
+    auto inside = [&](int J, int s) { return !GEN || 16 * J + 2 * s + g < C; };
+    // May these exponents' planes not be summed?
+    auto is_far = [&](const int (&e)[Q]) {
+        constexpr int kSpread = Q == 1 ? 127 : Q == 2 ? 10 : Q <= 4 ? 9 : 8;
+        int hi = e[0], lo = e[0];
+#pragma unroll
+        for (int i = 1; i < Q; ++i) {
+            hi = max(hi, e[i]);
+            lo = imin(lo, e[i]);
+        }
+        return hi > 0 || lo < -14 || hi - lo > kSpread;
+    };
+    // one block: w(i, h) plane i's key word of steps 4 h .. 4 h + 3, e(i, s) its exponent
+    auto summed = [&](int J, const uint4* xs, auto w, auto e) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            half8_t W[4];
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                half2_t p[2][4];
+                Factor f[2][Q];
+#pragma unroll
+                for (int o = 0; o < 2; ++o) {
+                    half2_t sum;
+#pragma unroll
+                    for (int i = 0; i < Q; ++i) {
+                        const int s = 4 * h + 2 * u + o;
+                        f[o][i] = factor(e(i, s));
+                        if (Q > 4 || GEN) {
+                            const half2_t z = both(i < a.q && inside(J, s) ? 1.0f : 0.0f);
+                            f[o][i] = {f[o][i].m10 * z, f[o][i].m12 * z, f[o][i].m14 * z};
+                        }
+                        sum = i == 0 ? -f[o][i].m14 : sum - f[o][i].m14;
+                    }
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) p[o][j] = sum;
+                }
+#pragma unroll
+                for (int i = 0; i < Q; ++i) {
+                    const Spread sp = spread(w(i, h), u);
+#pragma unroll
+                    for (int o = 0; o < 2; ++o)
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) p[o][j] = add_pair(sp, f[o][i], o, j, p[o][j]);
+                }
+                W[2 * u] = cat(p[0]);
+                W[2 * u + 1] = cat(p[1]);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            // activations are read kAhead products before they are used
+            int xw = x_word;
+            asm volatile("" : "+v"(xw));  // (addresses are not kept over the blocks)
+            constexpr int kAhead = CT > 2 ? 4 : 2 * CT, kRing = kAhead + 1;
+            half8_t X[kRing];
+            auto read = [&](int q) {
+                const int s = 4 * h + q / CT, c = q % CT;
+                X[q % kRing] =
+                    __builtin_bit_cast(half8_t, xs[512 * c + ((2 * s) ^ xw)]);
+            };
+#pragma unroll
+            for (int q = 0; q < kAhead; ++q) read(q);
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int q = 0; q < 4 * CT; ++q) {
+                if (q + kAhead < 4 * CT) read(q + kAhead);
+                acc[q % CT] = __builtin_amdgcn_mfma_f32_32x32x16_f16(W[q / CT], X[q % kRing],
+                                                                     acc[q % CT], 0, 0, 0);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        }
+    };
+    // Any exponents: a product a plane in bfloat16, whose range holds +-2^e, with the
+    // activations as two exact pieces.
+    auto plane_by_plane = [&](int J, const uint4* xs, auto w, auto e) {
+        uint64_t keys[Q], ex[Q];  // a byte per step, the next one lowest
+#pragma unroll
+        for (int i = 0; i < Q; ++i) {
+            keys[i] = (uint64_t)w(i, 1) << 32 | w(i, 0);
+            ex[i] = 0;
+#pragma unroll
+            for (int s = 0; s < (GEN ? 8 : 1); ++s)
+                ex[i] |= (uint64_t)(uint8_t)e(i, s) << (8 * s);
+        }
+#pragma unroll 1
+        for (int s = 0; s < 8; ++s) {
+            bhalf8_t W[Q];
+#pragma unroll
+            for (int i = 0; i < Q; ++i) {
+                const Spread sp = spread((uint32_t)keys[i], 0);
+                const int ei = (int)(int8_t)ex[i];
+                // 2^-127 and 2^-128 are subnormal
+                uint32_t mag = ei > -127 ? (uint32_t)(ei + 127) << 7 : ei == -127 ? 0x40u : 0x20u;
+                mag |= mag << 16;
+                const bool none = i >= a.q || !inside(J, s);
+                uint32_t p[4];
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    p[j] = none ? 0u : ((sp.v << (15 - 2 * j)) & 0x80008000u) ^ (mag | 0x80008000u);
+                W[i] = __builtin_bit_cast(bhalf8_t, uint4{p[0], p[1], p[2], p[3]});
+                keys[i] >>= 8;
+                if constexpr (GEN) ex[i] >>= 8;
+            }
+#pragma unroll
+            for (int c = 0; c < CT; ++c) {
+                const half8_t X = __builtin_bit_cast(half8_t, xs[512 * c + ((2 * s) ^ x_word)]);
+                uint32_t hi[4], lo[4];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    // eight significant bits, and the at most three behind them
+                    const float f0 = (float)X[2 * j], f1 = (float)X[2 * j + 1];
+                    const uint32_t h0 = __builtin_bit_cast(uint32_t, f0) & 0xffff0000u;
+                    const uint32_t h1 = __builtin_bit_cast(uint32_t, f1) & 0xffff0000u;
+                    const float l0 = f0 - __builtin_bit_cast(float, h0);
+                    const float l1 = f1 - __builtin_bit_cast(float, h1);
+                    hi[j] = h0 >> 16 | h1;
+                    lo[j] = __builtin_bit_cast(uint32_t, l0) >> 16 |
+                            (__builtin_bit_cast(uint32_t, l1) & 0xffff0000u);
+                }
+                const bhalf8_t H = __builtin_bit_cast(bhalf8_t, uint4{hi[0], hi[1], hi[2], hi[3]});
+                const bhalf8_t L = __builtin_bit_cast(bhalf8_t, uint4{lo[0], lo[1], lo[2], lo[3]});
+#pragma unroll
+                for (int i = 0; i < Q; ++i) {
+                    acc[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(W[i], H, acc[c], 0, 0, 0);
+                    acc[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(W[i], L, acc[c], 0, 0, 0);
+                }
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        }
+    };
+
+    Keys<Q, GEN> k;
+    if (blk0 < blk1) {
+        copy_x(blk0, 0);
+        load_keys(blk0, k);
+    }
+    arrive();
+    if constexpr (GEN) {
+#pragma unroll 1
+        for (int s = 0; s < steps; ++s) {
+            const int J = blk0 + s;
+            if (J + 1 < blk1) copy_x(J + 1, (s + 1) & 1);
+            if (J < blk1) {
+                const Keys<Q, GEN> now = k;
+                if (J + 1 < blk1) load_keys(J + 1, k);
+                auto w = [&](int i, int h) { return h ? now.w[i].y : now.w[i].x; };
+                auto e = [&](int i, int st) {
+                    return (int)(int8_t)((st & 4 ? now.w[i].w : now.w[i].z) >> (8 * (st & 3)));
+                };
+                bool far = false;
+#pragma unroll
+                for (int st = 0; st < 8; ++st) {
+                    int ex[Q];
+#pragma unroll
+                    for (int i = 0; i < Q; ++i) ex[i] = e(i, st);
+                    far |= is_far(ex);
+                }
+                const uint4* xs = xr + (s & 1) * kBuf;
+                if (__any(far)) plane_by_plane(J, xs, w, e);
+                else summed(J, xs, w, e);
+            }
+            arrive();
+        }
+    } else {
+        // groups of two blocks; the next group's keys are requested in the second
+#pragma unroll 1
+        for (int s0 = 0; s0 < steps; s0 += 2) {
+            uint32_t wd[2][Q][2], ew[2][kE];  // [block]
+            bool far = false;
+            if (blk0 + s0 < blk1) {
+                const uint32_t rot = 16u - (uint32_t)(n & 15);
+                int ex[Q];
+                uint32_t own[kE] = {};
+#pragma unroll
+                for (int i = 0; i < Q; ++i) {
+                    uint32_t c[4];
+                    rotate16(k.w[i], (int)rot, c);
+                    // even and odd chunks; lanes 0-31 keep the even ones of both blocks
+                    uint32_t ev[2], od[2];
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        ev[h] = __builtin_amdgcn_perm(c[2 * h + 1], c[2 * h], 0x06040200u);
+                        od[h] = __builtin_amdgcn_perm(c[2 * h + 1], c[2 * h], 0x07050301u);
+                        const auto sw = __builtin_amdgcn_permlane32_swap(ev[h], od[h], false, false);
+                        wd[0][i][h] = sw[0];
+                        wd[1][i][h] = sw[1];
+                    }
+                    ex[i] = (int)(int8_t)k.e[i];
+                    own[i >> 2] |= k.e[i] << (8 * (i & 3));
+                }
+                far = is_far(ex);
+#pragma unroll
+                for (int d = 0; d < kE; ++d) {
+                    const auto sw = __builtin_amdgcn_permlane32_swap(own[d], own[d], false, false);
+                    ew[0][d] = sw[0];
+                    ew[1][d] = sw[1];
+                }
+            }
+            const bool sum = !__any(far);
+            auto step = [&](auto bc) {
+                constexpr int b = decltype(bc)::value;
+                const int J = blk0 + s0 + b;
+                if (s0 + b >= steps) return;
+                if (J + 1 < blk1) copy_x(J + 1, (b + 1) & 1);
+                if (b == 1 && J + 1 < blk1) load_keys(J + 1, k);
+                if (J < blk1) {
+                    auto w = [&](int i, int h) { return wd[b][i][h]; };
+                    auto e = [&](int i, int) { return (int)(int8_t)(ew[b][i >> 2] >> (8 * (i & 3))); };
+                    const uint4* xs = xr + b * kBuf;
+                    if (sum) summed(J, xs, w, e);
+                    else plane_by_plane(J, xs, w, e);
+                }
+                arrive();
+            };
+            step(std::integral_constant<int, 0>{});
+            step(std::integral_constant<int, 1>{});
+        }
+    }
+
+    // Through LDS to outputs: lane (r, g) of row tile c has row r of it and 16 consecutive
+    // outputs from nb.  Loops that are not unrolled: what follows the product is a lot of
+    // code.  KW = 1: a wave's own space takes half its row tiles at a time.
+    constexpr int kPasses = KW > 1 ? 1 : 2, kPass = CT / kPasses;
+    constexpr int kVals = kPass * 1024;
+    static_assert(CT % kPasses == 0 && kWaves * kVals <= KW * 2 * kBuf * 4, "sums fit the buffers");
+    float* red = reinterpret_cast<float*>(xbuf) + lane;
+    const int nb = n0 + 16 * g;
+    sa_epi::Epilogue epi = a.epi;
+    if (epi.bias) epi.bias += (int64_t)expert * N;
+#pragma unroll
+    for (int pass = 0; pass < kPasses; ++pass) {
+#pragma unroll
+        for (int c = 0; c < kPass; ++c)
+#pragma unroll
+            for (int v = 0; v < 16; ++v)
+                red[wave * kVals + (c * 16 + v) * 64] = acc[pass * kPass + c][v];
+        if constexpr (KW > 1) __syncthreads();
+        else wave_fence();
+#pragma unroll 1
+        for (int o = KW > 1 ? kw : 0; o < 2 * kPass; o += KW) {
+            const int c = o >> 1, nn = nb + 8 * (o & 1);
+            const int row = first + kTile * (pass * kPass + c) + r;
+            if (row >= end || nn >= N || sa_linear::source_row(a, row) < 0) continue;
+            float v[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const float* p = red + rw * kVals + (o * 8 + j) * 64;
+                v[j] = p[0];
+#pragma unroll
+                for (int u = 1; u < KW; ++u) v[j] += p[u * RW * kVals];
+            }
+            const int64_t at = (int64_t)row * N + nn;
+            if (pa.vector_out) sa_epi::finish_vector<8>(epi, at, nn, v);
+            else sa_epi::finish_some<8>(epi, at, nn, N - nn, v);
+        }
+        if constexpr (kPasses > 1) wave_fence();
+    }
+}
+
+template <int Q, int CT, int KW, bool GEN>
+__global__ __launch_bounds__(kThreads, 2) void k_panel(Args pa) {
+    __shared__ uint4 xbuf[KW * 2 * CT * 512];
+    body<Q, CT, KW, GEN>(pa, xbuf);
+}
+
+template <int Q, int CT, int KW, bool GEN>
+void start(Args& pa, hipStream_t s) {
+    const int cols = kTile * (kWaves / KW);
+    pa.n_tiles = (pa.a.N + cols - 1) / cols;
+    pa.vector_out = pa.a.N % 8 == 0;
+    const int64_t tiles = sa_linear::most_tiles(pa.a, kTile * CT);
+    hipLaunchKernelGGL((k_panel<Q, CT, KW, GEN>), dim3((unsigned)(tiles * pa.n_tiles)),
+                       dim3(kThreads), 0, s, pa);
+}
+
+template <int Q>
+void start_tiles(Args& pa, int ct, hipStream_t s) {
+    if (ct == 8) start<Q, 8, 1, false>(pa, s);
+    else if (ct == 4) start<Q, 4, 1, false>(pa, s);
+    else if (ct == 2) start<Q, 2, 2, false>(pa, s);
+    else start<Q, 1, 4, false>(pa, s);
+}
+
+}  // namespace
+
+void launch(const Layer& a, hipStream_t s) {
+    Args pa{};
+    pa.a = a;
+    const uint32_t d = (uint32_t)(a.G / 128);
+    pa.group_magic = d <= 1 ? 0u : (uint32_t)(((1ull << 32) + d - 1) / d);
+    const int per = a.offsets ? (a.rows + a.experts - 1) / a.experts : a.rows;
+    const int ct = per > 512 ? 8 : per > 128 ? 4 : per > 32 ? 2 : 1;
+    // blocks to groups by multiplication: up to 2^22 columns
+    if (a.G % 128 || a.K > (1 << 22)) {
+        if (a.q > 4) start<8, 1, 4, true>(pa, s);
+        else if (ct >= 4) start<4, 4, 1, true>(pa, s);
+        else start<4, 1, 4, true>(pa, s);
+        return;
+    }
+    switch (a.q) {
+        case 1: start_tiles<1>(pa, ct, s); break;
+        case 2: start_tiles<2>(pa, ct, s); break;
+        case 3: start_tiles<3>(pa, ct, s); break;
+        case 4: start_tiles<4>(pa, ct, s); break;
+        default: start<8, 2, 2, false>(pa, s); break;
+    }
+}
+
+}  // namespace sa_panel

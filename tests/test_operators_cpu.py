@@ -26,6 +26,8 @@ def experts(x=A, x_rows=8, row_of=None, off=A, p=A, e=A, q=3, N=64, K=256, G=128
     (dict(q=0), Q), (dict(q=9), Q), (dict(N=0), SHAPE), (dict(K=12), SHAPE), (dict(K=0), SHAPE),
     (dict(rows=-1), SHAPE), (dict(rows=sa.SA_MAX_ROWS + 1), SHAPE),
     (dict(rows=sa.SA_MAX_ROWS, N=1 << 15), SHAPE),   # 2^35 outputs
+    (dict(rows=1, N=1 << 28, K=8, G=8), SHAPE),       # 2^23 columns of tiles
+    (dict(rows=sa.SA_MAX_ROWS, K=1 << 16), SHAPE),    # 2^36 activations
     (dict(act=-1), SHAPE), (dict(act=5), SHAPE),
     (dict(G=0), GROUP), (dict(G=12), GROUP), (dict(G=96), GROUP),
     (dict(x=A + 8), ALIGN), (dict(p=A + 4), ALIGN), (dict(y=A + 8), ALIGN),
