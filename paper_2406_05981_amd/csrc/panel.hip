@@ -8,8 +8,8 @@
 // planes is exact and one matrix product serves all planes.  (Below -14 the sum may
 // be subnormal, and the matrix core then drops low bits of its products: measured
 // 7e-6 of sum|terms| at 2^-24.)  A block of 128 columns
-// that has any other exponents in a wave's rows takes two products a plane: +-2^e is a
-// bfloat16 number, an activation the sum of two.
+// that has any other exponents in a wave's rows is left for a second loop, two products a
+// plane: +-2^e is a bfloat16 number, an activation the sum of two.
 #include <hip/hip_runtime.h>
 
 #include <type_traits>
@@ -337,7 +337,53 @@ __device__ __forceinline__ void body(const Args& pa, uint4* xbuf) {
         }
     };
 
+    // A group of two blocks as words in step order: wd[block][plane][half], ew the planes'
+    // exponents of a block; returns whether this lane's row has a block to do plane by plane.
+    auto unpack = [&](const Keys<Q, GEN>& k, uint32_t (&wd)[2][Q][2], uint32_t (&ew)[2][kE]) {
+        int ex[Q];
+        uint32_t own[kE] = {};
+#pragma unroll
+        for (int i = 0; i < Q; ++i) {
+            uint32_t c[4];
+            rotate16(k.w[i], 16 - (n & 15), c);
+            // even and odd chunks; lanes 0-31 keep the even ones of both blocks
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const uint32_t ev = __builtin_amdgcn_perm(c[2 * h + 1], c[2 * h], 0x06040200u);
+                const uint32_t od = __builtin_amdgcn_perm(c[2 * h + 1], c[2 * h], 0x07050301u);
+                const auto sw = __builtin_amdgcn_permlane32_swap(ev, od, false, false);
+                wd[0][i][h] = sw[0];
+                wd[1][i][h] = sw[1];
+            }
+            ex[i] = (int)(int8_t)k.e[i];
+            own[i >> 2] |= k.e[i] << (8 * (i & 3));
+        }
+#pragma unroll
+        for (int d = 0; d < kE; ++d) {
+            const auto sw = __builtin_amdgcn_permlane32_swap(own[d], own[d], false, false);
+            ew[0][d] = sw[0];
+            ew[1][d] = sw[1];
+        }
+        return is_far(ex);
+    };
+    auto word_of = [](const Keys<Q, GEN>& k, int i, int h) { return h ? k.w[i].y : k.w[i].x; };
+    auto exponent_of = [](const Keys<Q, GEN>& k, int i, int s) {
+        return (int)(int8_t)((s & 4 ? k.w[i].w : k.w[i].z) >> (8 * (s & 3)));
+    };
+    auto block_far = [&](const Keys<Q, GEN>& k) {
+        bool far = false;
+#pragma unroll
+        for (int s = 0; s < 8; ++s) {
+            int ex[Q];
+#pragma unroll
+            for (int i = 0; i < Q; ++i) ex[i] = exponent_of(k, i, s);
+            far |= is_far(ex);
+        }
+        return far;
+    };
+
     Keys<Q, GEN> k;
+    bool left = false;  // blocks were left for the second loop
     if (blk0 < blk1) {
         copy_x(blk0, 0);
         load_keys(blk0, k);
@@ -351,21 +397,12 @@ __device__ __forceinline__ void body(const Args& pa, uint4* xbuf) {
             if (J < blk1) {
                 const Keys<Q, GEN> now = k;
                 if (J + 1 < blk1) load_keys(J + 1, k);
-                auto w = [&](int i, int h) { return h ? now.w[i].y : now.w[i].x; };
-                auto e = [&](int i, int st) {
-                    return (int)(int8_t)((st & 4 ? now.w[i].w : now.w[i].z) >> (8 * (st & 3)));
-                };
-                bool far = false;
-#pragma unroll
-                for (int st = 0; st < 8; ++st) {
-                    int ex[Q];
-#pragma unroll
-                    for (int i = 0; i < Q; ++i) ex[i] = e(i, st);
-                    far |= is_far(ex);
-                }
-                const uint4* xs = xr + (s & 1) * kBuf;
-                if (__any(far)) plane_by_plane(J, xs, w, e);
-                else summed(J, xs, w, e);
+                if (__any(block_far(now)))
+                    left = true;
+                else
+                    summed(J, xr + (s & 1) * kBuf,
+                           [&](int i, int h) { return word_of(now, i, h); },
+                           [&](int i, int st) { return exponent_of(now, i, st); });
             }
             arrive();
         }
@@ -373,55 +410,52 @@ __device__ __forceinline__ void body(const Args& pa, uint4* xbuf) {
         // groups of two blocks; the next group's keys are requested in the second
 #pragma unroll 1
         for (int s0 = 0; s0 < steps; s0 += 2) {
-            uint32_t wd[2][Q][2], ew[2][kE];  // [block]
-            bool far = false;
-            if (blk0 + s0 < blk1) {
-                const uint32_t rot = 16u - (uint32_t)(n & 15);
-                int ex[Q];
-                uint32_t own[kE] = {};
-#pragma unroll
-                for (int i = 0; i < Q; ++i) {
-                    uint32_t c[4];
-                    rotate16(k.w[i], (int)rot, c);
-                    // even and odd chunks; lanes 0-31 keep the even ones of both blocks
-                    uint32_t ev[2], od[2];
-#pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        ev[h] = __builtin_amdgcn_perm(c[2 * h + 1], c[2 * h], 0x06040200u);
-                        od[h] = __builtin_amdgcn_perm(c[2 * h + 1], c[2 * h], 0x07050301u);
-                        const auto sw = __builtin_amdgcn_permlane32_swap(ev[h], od[h], false, false);
-                        wd[0][i][h] = sw[0];
-                        wd[1][i][h] = sw[1];
-                    }
-                    ex[i] = (int)(int8_t)k.e[i];
-                    own[i >> 2] |= k.e[i] << (8 * (i & 3));
-                }
-                far = is_far(ex);
-#pragma unroll
-                for (int d = 0; d < kE; ++d) {
-                    const auto sw = __builtin_amdgcn_permlane32_swap(own[d], own[d], false, false);
-                    ew[0][d] = sw[0];
-                    ew[1][d] = sw[1];
-                }
-            }
-            const bool sum = !__any(far);
+            uint32_t wd[2][Q][2], ew[2][kE];
+            const bool far = __any(unpack(k, wd, ew) && blk0 + s0 + g < blk1);
+            left |= far;
             auto step = [&](auto bc) {
                 constexpr int b = decltype(bc)::value;
                 const int J = blk0 + s0 + b;
                 if (s0 + b >= steps) return;
                 if (J + 1 < blk1) copy_x(J + 1, (b + 1) & 1);
                 if (b == 1 && J + 1 < blk1) load_keys(J + 1, k);
-                if (J < blk1) {
-                    auto w = [&](int i, int h) { return wd[b][i][h]; };
-                    auto e = [&](int i, int) { return (int)(int8_t)(ew[b][i >> 2] >> (8 * (i & 3))); };
-                    const uint4* xs = xr + b * kBuf;
-                    if (sum) summed(J, xs, w, e);
-                    else plane_by_plane(J, xs, w, e);
-                }
+                if (J < blk1 && !far)
+                    summed(J, xr + b * kBuf, [&](int i, int h) { return wd[b][i][h]; },
+                           [&](int i, int) { return (int)(int8_t)(ew[b][i >> 2] >> (8 * (i & 3))); });
                 arrive();
             };
             step(std::integral_constant<int, 0>{});
             step(std::integral_constant<int, 1>{});
+        }
+    }
+    // the second loop runs the groups that the first one left, the same in every way
+    if (__syncthreads_or(left)) {
+#pragma unroll 1
+        for (int s = 0; s < steps; ++s) {
+            const int J = blk0 + s;
+            if (J < blk1) copy_x(J, 0);
+            arrive();
+            if (J < blk1) {
+                if constexpr (GEN) {
+                    load_keys(J, k);
+                    if (__any(block_far(k)))
+                        plane_by_plane(J, xr, [&](int i, int h) { return word_of(k, i, h); },
+                                       [&](int i, int st) { return exponent_of(k, i, st); });
+                } else {
+                    uint32_t wd[2][Q][2], ew[2][kE];
+                    load_keys(J & ~1, k);
+                    if (__any(unpack(k, wd, ew) && (J & ~1) + g < blk1)) {
+                        const bool b = J & 1;
+                        plane_by_plane(J, xr,
+                                       [&](int i, int h) { return b ? wd[1][i][h] : wd[0][i][h]; },
+                                       [&](int i, int) {
+                                           const uint32_t ei = b ? ew[1][i >> 2] : ew[0][i >> 2];
+                                           return (int)(int8_t)(ei >> (8 * (i & 3)));
+                                       });
+                    }
+                }
+            }
+            __syncthreads();
         }
     }
 
