@@ -62,66 +62,66 @@ __device__ inline void store(void* p, int64_t i, float v, int half) {
     else static_cast<float*>(p)[i] = v;
 }
 
-// V (4 or 8) consecutive outputs of one row from element i, a multiple of V.
-template <int V>
-__device__ inline void load_vector(const void* p, int64_t i, int half, float (&out)[V]) {
-    typedef _Float16 halfv_t __attribute__((ext_vector_type(V)));
-    typedef float floatv_t __attribute__((ext_vector_type(V)));
-    if (half) {
-        const halfv_t h = *reinterpret_cast<const halfv_t*>(static_cast<const _Float16*>(p) + i);
-#pragma unroll
-        for (int j = 0; j < V; ++j) out[j] = (float)h[j];
-    } else {
-        const floatv_t f = *reinterpret_cast<const floatv_t*>(static_cast<const float*>(p) + i);
-#pragma unroll
-        for (int j = 0; j < V; ++j) out[j] = f[j];
-    }
-}
-
-template <int V>
-__device__ inline void finish_vector(const Epilogue& e, int64_t i, int n, float (&v)[V]) {
-    typedef _Float16 halfv_t __attribute__((ext_vector_type(V)));
-    typedef float floatv_t __attribute__((ext_vector_type(V)));
-    float z[V];
-    if (e.bias) {
-#pragma unroll
-        for (int j = 0; j < V; ++j) v[j] += e.bias[n + j];
-    }
-    activate(v, e.act);
-    if (e.multiplier) {
-        load_vector<V>(e.multiplier, i, e.half, z);
-#pragma unroll
-        for (int j = 0; j < V; ++j) v[j] *= z[j];
-    }
-    if (e.residual) {
-        load_vector<V>(e.residual, i, e.half, z);
-#pragma unroll
-        for (int j = 0; j < V; ++j) v[j] += z[j];
-    }
+// 8 consecutive outputs of one row from element i.  Their operands are requested as they
+// lie in memory (rows of odd lengths begin at any element) and unpacked when they are used.
+typedef _Float16 half8_t __attribute__((ext_vector_type(8), aligned(2)));
+typedef float float8_t __attribute__((ext_vector_type(8), aligned(4)));
+struct Operands8 {
+    half8_t multiplier_h, residual_h;
+    float8_t multiplier_f, residual_f;
+};
+__device__ inline void fetch(const Epilogue& e, int64_t i, Operands8* o) {
     if (e.half) {
-        halfv_t h;
-#pragma unroll
-        for (int j = 0; j < V; ++j) h[j] = (_Float16)v[j];
-        *reinterpret_cast<halfv_t*>(static_cast<_Float16*>(e.y) + i) = h;
+        if (e.multiplier)
+            o->multiplier_h =
+                *reinterpret_cast<const half8_t*>(static_cast<const _Float16*>(e.multiplier) + i);
+        if (e.residual)
+            o->residual_h =
+                *reinterpret_cast<const half8_t*>(static_cast<const _Float16*>(e.residual) + i);
     } else {
-        floatv_t f;
-#pragma unroll
-        for (int j = 0; j < V; ++j) f[j] = v[j];
-        *reinterpret_cast<floatv_t*>(static_cast<float*>(e.y) + i) = f;
+        if (e.multiplier)
+            o->multiplier_f =
+                *reinterpret_cast<const float8_t*>(static_cast<const float*>(e.multiplier) + i);
+        if (e.residual)
+            o->residual_f =
+                *reinterpret_cast<const float8_t*>(static_cast<const float*>(e.residual) + i);
     }
 }
 
-// The first `count` of V consecutive outputs of one row from element i.
-template <int V>
-__device__ inline void finish_some(const Epilogue& e, int64_t i, int n, int count, float (&v)[V]) {
-    if (e.bias) {
+__device__ inline void finish(const Epilogue& e, int64_t i, const float (&bias)[8],
+                              const Operands8& o, float (&v)[8]) {
 #pragma unroll
-        for (int j = 0; j < V; ++j)
-            if (j < count) v[j] += e.bias[n + j];
+    for (int j = 0; j < 8; ++j) v[j] += bias[j];
+    activate(v, e.act);
+    if (e.half) {
+        half8_t h;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            if (e.multiplier) v[j] *= (float)o.multiplier_h[j];
+            if (e.residual) v[j] += (float)o.residual_h[j];
+            h[j] = (_Float16)v[j];
+        }
+        *reinterpret_cast<half8_t*>(static_cast<_Float16*>(e.y) + i) = h;
+    } else {
+        float8_t f;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            if (e.multiplier) v[j] *= o.multiplier_f[j];
+            if (e.residual) v[j] += o.residual_f[j];
+            f[j] = v[j];
+        }
+        *reinterpret_cast<float8_t*>(static_cast<float*>(e.y) + i) = f;
     }
+}
+
+// The first `count` of 8 such outputs.
+__device__ inline void finish_some(const Epilogue& e, int64_t i, const float (&bias)[8], int count,
+                                   float (&v)[8]) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] += bias[j];
     activate(v, e.act);
 #pragma unroll
-    for (int j = 0; j < V; ++j) {
+    for (int j = 0; j < 8; ++j) {
         if (j >= count) break;
         if (e.multiplier) v[j] *= load(e.multiplier, i + j, e.half);
         if (e.residual) v[j] += load(e.residual, i + j, e.half);
@@ -129,10 +129,18 @@ __device__ inline void finish_some(const Epilogue& e, int64_t i, int n, int coun
     }
 }
 
-// One output: element i = row * N + n.
-__device__ inline void finish(const Epilogue& e, int64_t i, int n, float v) {
-    float one[1] = {v};
-    finish_some(e, i, n, 1, one);
+// One output: what it needs besides its sum may be requested before the sum is there.
+struct Operands {
+    float bias, multiplier, residual;
+};
+__device__ inline Operands fetch(const Epilogue& e, int64_t i, int n) {
+    return {e.bias ? e.bias[n] : 0.0f, e.multiplier ? load(e.multiplier, i, e.half) : 1.0f,
+            e.residual ? load(e.residual, i, e.half) : 0.0f};
+}
+__device__ inline void finish(const Epilogue& e, int64_t i, const Operands& o, float v) {
+    float z[1] = {v + o.bias};
+    activate(z, e.act);
+    store(e.y, i, fmaf(z[0], o.multiplier, o.residual), e.half);
 }
 
 }  // namespace sa_epi

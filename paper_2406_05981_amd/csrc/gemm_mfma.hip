@@ -34,6 +34,7 @@
 // 88 us.
 #include "gemm_matrix.h"
 #include "keys.h"
+#include "linear.h"
 
 namespace sa_mfma {
 namespace {
@@ -163,8 +164,10 @@ struct Group {
 // lane and then between the lane groups, in registers.  The block loop stays
 // rolled: its code runs four times a group and would be fetched cold.  The next group's keys are requested
 // before the current group's products; activations one block ahead.
-template <int Q, int RT, bool ADD>
-__device__ __forceinline__ void split_body(const KernelArgs& ka, float* red) {
+// EPI: the outputs are the epilogue's.
+template <int Q, int RT, bool ADD, bool EPI = false>
+__device__ __forceinline__ void split_body(const KernelArgs& ka, float* red,
+                                           const sa_epi::Epilogue& epi = sa_epi::Epilogue{}) {
     const Args& a = ka.a;
     constexpr int kE = ADD ? 4 : 1;
     const int C = a.K >> 3, C16 = C >> 4, NG = ka.NG;
@@ -359,7 +362,10 @@ __device__ __forceinline__ void split_body(const KernelArgs& ka, float* red) {
             const float* p = red + set * ka.ksplit * kVals + q;
             float s = p[0];
             for (int w = 1; w < ka.ksplit; ++w) s += p[w * kVals];
-            if (a.out_half)
+            if constexpr (EPI) {
+                const int64_t at = (int64_t)b * a.N + row;
+                sa_epi::finish(epi, at, sa_epi::fetch(epi, at, row), s);
+            } else if (a.out_half)
                 static_cast<uint16_t*>(a.y)[(int64_t)b * a.N + row] =
                     __builtin_bit_cast(uint16_t, (_Float16)s);
             else
@@ -373,6 +379,14 @@ __global__ __launch_bounds__(kThreads, RT == 1 && Q <= (ADD ? 2 : 3) ? 4 : 2)
 void k_gemm_split(KernelArgs a) {
     __shared__ float red[kWaves * RT * 256];
     split_body<Q, RT, ADD>(a, red);
+}
+
+// The row-wise layer with an epilogue.
+template <int Q, int RT>
+__global__ __launch_bounds__(kThreads, RT == 1 && Q <= 3 ? 4 : 2)
+void k_gemm_split_epilogue(KernelArgs a, sa_epi::Epilogue epi) {
+    __shared__ float red[kWaves * RT * 256];
+    split_body<Q, RT, false, true>(a, red, epi);
 }
 
 // ---------------------------------------------------------------- activations shared in LDS
@@ -611,6 +625,21 @@ void launch_split(const KernelArgs& ka, int grid, hipStream_t s) {
     }
 }
 
+template <int RT>
+void launch_split_epilogue(const KernelArgs& ka, const sa_epi::Epilogue& e, int grid,
+                           hipStream_t s) {
+    const dim3 g(grid), b(kThreads);
+    switch (ka.a.q) {
+        case 1: hipLaunchKernelGGL((k_gemm_split_epilogue<1, RT>), g, b, 0, s, ka, e); break;
+        case 2: hipLaunchKernelGGL((k_gemm_split_epilogue<2, RT>), g, b, 0, s, ka, e); break;
+        case 3: hipLaunchKernelGGL((k_gemm_split_epilogue<3, RT>), g, b, 0, s, ka, e); break;
+        default:
+            if constexpr (RT <= 3)
+                hipLaunchKernelGGL((k_gemm_split_epilogue<4, RT>), g, b, 0, s, ka, e);
+            break;
+    }
+}
+
 template <int CT, int RW>
 void launch_tile(const KernelArgs& ka, int grid, hipStream_t s) {
     const dim3 g(grid), b(kTileThreads);
@@ -634,7 +663,8 @@ void launch_tile(const KernelArgs& ka, int grid, hipStream_t s) {
 // (its activations are requested one 128-column block ahead), more of them on a CU
 // their issue time.  Tile: the same per 128-column block of a column share.
 // Row tiles that spill (4 planes x 4 tiles, additive 4 x 2) are left out.
-double plan(int q, int N, int K, int G, int B, int terms, sa_matrix_plan* p) {
+static double plan_kernels(int q, int N, int K, int G, int B, int terms, bool tile,
+                           sa_matrix_plan* p) {
     *p = sa_matrix_plan{};
     const bool add = terms > 0;
     if (K > (1 << 22) || (add && B < 5)) return sa_matrix::kNever;
@@ -684,7 +714,7 @@ double plan(int q, int N, int K, int G, int B, int terms, sa_matrix_plan* p) {
         offer(add ? 1.09 * us : us, 2, rt, 1, ksplit, rows, kThreads,
               sizeof(float) * kWaves * rt * 256);
     }
-    if (add) return best;
+    if (add || !tile) return best;
     struct Fit {
         int ct, rw;
         double base, alone, alone_q, shared, shared_q;
@@ -705,7 +735,15 @@ double plan(int q, int N, int K, int G, int B, int terms, sa_matrix_plan* p) {
     return best;
 }
 
-void launch(const Args& a, const sa_matrix_plan& p, hipStream_t s) {
+double plan(int q, int N, int K, int G, int B, int terms, sa_matrix_plan* p) {
+    return plan_kernels(q, N, K, G, B, terms, true, p);
+}
+
+double plan_split(const sa_linear::Layer& l, sa_matrix_plan* p) {
+    return plan_kernels(l.q, l.N, l.K, l.G, l.rows, 0, false, p);
+}
+
+static KernelArgs kernel_args(const Args& a, const sa_matrix_plan& p) {
     const bool add = a.terms > 0;
     KernelArgs ka{};
     ka.a = a;
@@ -717,6 +755,21 @@ void launch(const Args& a, const sa_matrix_plan& p, hipStream_t s) {
     const uintptr_t e = reinterpret_cast<uintptr_t>(a.exps) |
                         (add ? reinterpret_cast<uintptr_t>(a.term_signs) : 0);
     ka.vec = a.G == 128 && a.K % 512 == 0 && (e & (add ? 7u : 3u)) == 0 && (!add || a.terms == 2);
+    return ka;
+}
+
+void launch(const sa_linear::Layer& l, const sa_matrix_plan& p, hipStream_t s) {
+    const KernelArgs ka = kernel_args({l.x, l.packed, l.exps, nullptr, l.q, l.N, l.K, l.G, l.rows, 0,
+                                       l.epi.y, l.epi.half}, p);
+    if (p.row_tiles == 1) launch_split_epilogue<1>(ka, l.epi, p.workgroups, s);
+    else if (p.row_tiles == 2) launch_split_epilogue<2>(ka, l.epi, p.workgroups, s);
+    else if (p.row_tiles == 3) launch_split_epilogue<3>(ka, l.epi, p.workgroups, s);
+    else launch_split_epilogue<4>(ka, l.epi, p.workgroups, s);
+}
+
+void launch(const Args& a, const sa_matrix_plan& p, hipStream_t s) {
+    const bool add = a.terms > 0;
+    const KernelArgs ka = kernel_args(a, p);
     const int grid = p.workgroups;
     if (p.kernel == 3) {
         if (p.row_tiles == 4) {

@@ -40,6 +40,7 @@
 
 #include "gemm_matrix.h"
 #include "keys.h"
+#include "linear.h"
 
 namespace sa_mx {
 namespace {
@@ -75,6 +76,13 @@ struct KernelArgs {
     int sets;              // row sets of a workgroup: it has ksplit * sets waves
     int NG;                // exponent groups of a row
     uint32_t group_magic;  // sa_matrix::group_magic
+};
+
+// The rows of x and y of a call with an epilogue: batch row b is row first + b of y.
+struct Rows {
+    sa_epi::Epilogue epi;
+    const int32_t* row_of;  // row of x of each row of y, or null: the row itself
+    int first, x_rows;
 };
 
 // 32 signs as fp4 (e2m1) +-1.0: register v, nibble n holds bit 4n + v of the
@@ -168,9 +176,20 @@ struct Keys {
     uint32_t s[Q];  // additive: T term signs
 };
 
-template <int Q, int CT, int NP, bool ADD>
-__device__ __forceinline__ void body(const KernelArgs& ka, char* lds) {
+// EPI: the rows of `rows`, with its epilogue.
+template <int Q, int CT, int NP, bool ADD, bool EPI = false>
+__device__ __forceinline__ void body(const KernelArgs& ka, char* lds, int wg,
+                                     const Rows& rows = Rows{}) {
     const Args& a = ka.a;
+    // the row of x of batch row b; -1: none
+    auto source = [&](int b) {
+        if constexpr (EPI) {
+            if (!rows.row_of) return rows.first + b;
+            const int v = rows.row_of[rows.first + b];
+            return v >= 0 && v < rows.x_rows ? v : -1;
+        }
+        return b;
+    };
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     const int ksl = wave & (ka.ksplit - 1);
@@ -179,11 +198,14 @@ __device__ __forceinline__ void body(const KernelArgs& ka, char* lds) {
 
     // activations of this lane: 16 columns of batch rows (lane >> 5), + 2, + 4, ...
     const int xp = (lane >> 3) & 3, xm = (lane >> 1) & 3, xh = lane & 1;
+    int xrow[NP];
+#pragma unroll
+    for (int t = 0; t < NP; ++t) xrow[t] = imax(source(imin(2 * t + (lane >> 5), a.B - 1)), 0);
     auto load_x = [&](int jg, uint4 (&raw)[NP][2]) {
         const int64_t off = 128 * (int64_t)imin(kGroupBlocks * jg + xp, C16 - 1) + 16 * (lane & 7);
 #pragma unroll
         for (int t = 0; t < NP; ++t) {
-            const uint16_t* p = a.x + (int64_t)imin(2 * t + (lane >> 5), a.B - 1) * a.K + off;
+            const uint16_t* p = a.x + (int64_t)xrow[t] * a.K + off;
             raw[t][0] = *reinterpret_cast<const uint4*>(p);
             raw[t][1] = *reinterpret_cast<const uint4*>(p + 8);
         }
@@ -195,7 +217,7 @@ __device__ __forceinline__ void body(const KernelArgs& ka, char* lds) {
     const int r = lane & 15, g = lane >> 4;
     const int sets = ka.sets, rset = wave / ka.ksplit;
     // row tiles of this wave: the first `extra` shares take one more
-    const int share = (int)blockIdx.x * sets + rset;
+    const int share = wg * sets + rset;
     const int base = ka.tiles / ka.shares, extra = ka.tiles - base * ka.shares;
     const int ntiles = base + (share < extra ? 1 : 0);
     const int tile0 = share * base + imin(share, extra);
@@ -466,13 +488,14 @@ __device__ __forceinline__ void body(const KernelArgs& ka, char* lds) {
         ChunkList* list = reinterpret_cast<ChunkList*>(lds);
         for (int b = 0; b < a.B; ++b) {
             if (!__syncthreads_or((not_finite >> b) & 1u)) continue;
+            const uint16_t* xb = a.x + (int64_t)imax(source(b), 0) * a.K;
             for (int c0 = 0; c0 < C; c0 += (int)blockDim.x) {
                 if (threadIdx.x == 0) list->count = 0;
                 __syncthreads();
                 const int c = c0 + (int)threadIdx.x;
                 if (c < C) {
                     const uint32_t m = infinity_masks(
-                        *reinterpret_cast<const uint4*>(a.x + (int64_t)b * a.K + 8 * c));
+                        *reinterpret_cast<const uint4*>(xb + 8 * c));
                     if (m) list->chunk[atomicAdd(&list->count, 1u)] = {(uint32_t)c, m};
                 }
                 __syncthreads();
@@ -510,7 +533,11 @@ __device__ __forceinline__ void body(const KernelArgs& ka, char* lds) {
             const uint32_t f = (inf >> (2 * (o >> klog))) & 3u;
             if (f & 1u) y += __builtin_inff();
             if (f & 2u) y -= __builtin_inff();
-            if (a.out_half)
+            if constexpr (EPI) {
+                if (source(b) < 0) continue;
+                const int64_t at = (int64_t)(rows.first + b) * a.N + row;
+                sa_epi::finish(rows.epi, at, sa_epi::fetch(rows.epi, at, row), y);
+            } else if (a.out_half)
                 static_cast<uint16_t*>(a.y)[(int64_t)b * a.N + row] =
                     __builtin_bit_cast(uint16_t, (_Float16)y);
             else
@@ -529,7 +556,38 @@ constexpr int lds_bytes() {
 template <int Q, int CT, int NP, bool ADD>
 __global__ __launch_bounds__(kThreads, 2) void k_gemm_mx(KernelArgs a) {
     __shared__ uint4 lds[(lds_bytes<CT>() + 15) / 16];
-    body<Q, CT, NP, ADD>(a, reinterpret_cast<char*>(lds));
+    body<Q, CT, NP, ADD>(a, reinterpret_cast<char*>(lds), (int)blockIdx.x);
+}
+
+// The row-wise layer with an epilogue.
+template <int Q, int CT, int NP>
+__global__ __launch_bounds__(kThreads, 2) void k_gemm_mx_epilogue(KernelArgs a, Rows rows) {
+    __shared__ uint4 lds[(lds_bytes<CT>() + 15) / 16];
+    body<Q, CT, NP, false, true>(a, reinterpret_cast<char*>(lds), (int)blockIdx.x, rows);
+}
+
+// Experts of at most kExpertRows rows (the others are left to the panel kernel):
+// workgroups wgs * e ... have expert e, in the form for its number of rows.
+template <int Q>
+__global__ __launch_bounds__(kThreads, 2) void k_gemm_mx_experts(KernelArgs ka, Rows rows,
+                                                                 const int32_t* offsets, int slots,
+                                                                 int wgs) {
+    __shared__ uint4 lds[(lds_bytes<2>() + 15) / 16];
+    const int e = (int)(blockIdx.x / (unsigned)wgs), wg = (int)(blockIdx.x % (unsigned)wgs);
+    const int lo = imin(imax(offsets[e], 0), slots);
+    const int count = imin(imax(offsets[e + 1], lo), slots) - lo;
+    if (count < 1 || count > sa_mx::kExpertRows) return;
+    Args& a = ka.a;
+    const int64_t nk = (int64_t)a.q * a.N;
+    a.packed += e * nk * (a.K >> 3);
+    a.exps += e * nk * ka.NG;
+    a.B = count;
+    rows.first = lo;
+    if (rows.epi.bias) rows.epi.bias += (int64_t)e * a.N;
+    char* l = reinterpret_cast<char*>(lds);
+    if (count <= 2) body<Q, 1, 1, false, true>(ka, l, wg, rows);
+    else if (count <= 4) body<Q, 1, 2, false, true>(ka, l, wg, rows);
+    else body<Q, 2, 4, false, true>(ka, l, wg, rows);
 }
 
 // ---------------------------------------------------------------- choice and launch
@@ -542,6 +600,17 @@ void launch_q(const KernelArgs& ka, int grid, hipStream_t s) {
         case 2: hipLaunchKernelGGL((k_gemm_mx<2, CT, NP, ADD>), g, b, 0, s, ka); break;
         case 3: hipLaunchKernelGGL((k_gemm_mx<3, CT, NP, ADD>), g, b, 0, s, ka); break;
         default: hipLaunchKernelGGL((k_gemm_mx<4, CT, NP, ADD>), g, b, 0, s, ka); break;
+    }
+}
+
+template <int CT, int NP>
+void launch_epilogue(const KernelArgs& ka, const Rows& rows, int grid, hipStream_t s) {
+    const dim3 g(grid), b(64 * ka.ksplit * ka.sets);
+    switch (ka.a.q) {
+        case 1: hipLaunchKernelGGL((k_gemm_mx_epilogue<1, CT, NP>), g, b, 0, s, ka, rows); break;
+        case 2: hipLaunchKernelGGL((k_gemm_mx_epilogue<2, CT, NP>), g, b, 0, s, ka, rows); break;
+        case 3: hipLaunchKernelGGL((k_gemm_mx_epilogue<3, CT, NP>), g, b, 0, s, ka, rows); break;
+        default: hipLaunchKernelGGL((k_gemm_mx_epilogue<4, CT, NP>), g, b, 0, s, ka, rows); break;
     }
 }
 
@@ -600,7 +669,8 @@ double plan(int q, int N, int K, int G, int B, int terms, sa_matrix_plan* p) {
                       (f[5] + (1 - f[5]) * p->threads / kThreads) * (terms == 3 ? 1.12 : 1);
 }
 
-void launch(const Args& a, const sa_matrix_plan& p, hipStream_t s) {
+namespace {
+KernelArgs kernel_args(const Args& a, const sa_matrix_plan& p) {
     KernelArgs ka{};
     ka.a = a;
     ka.ksplit = p.column_shares;
@@ -609,8 +679,44 @@ void launch(const Args& a, const sa_matrix_plan& p, hipStream_t s) {
     ka.shares = p.workgroups * ka.sets;
     ka.NG = a.K / a.G;
     ka.group_magic = sa_matrix::group_magic(a.G);
+    return ka;
+}
+
+Args matrix_args(const sa_linear::Layer& l) {
+    return {l.x, l.packed, l.exps, nullptr, l.q, l.N, l.K, l.G, l.rows, 0, l.epi.y, l.epi.half};
+}
+}  // namespace
+
+void launch(const Args& a, const sa_matrix_plan& p, hipStream_t s) {
+    const KernelArgs ka = kernel_args(a, p);
     if (a.terms) launch_batch<true>(ka, p.workgroups, s);
     else launch_batch<false>(ka, p.workgroups, s);
+}
+
+void launch(const sa_linear::Layer& l, const sa_matrix_plan& p, hipStream_t s) {
+    const KernelArgs ka = kernel_args(matrix_args(l), p);
+    const Rows rows = {l.epi, l.row_of, 0, l.x_rows};
+    if (l.rows <= 2) launch_epilogue<1, 1>(ka, rows, p.workgroups, s);
+    else if (l.rows <= 4) launch_epilogue<1, 2>(ka, rows, p.workgroups, s);
+    else launch_epilogue<2, 4>(ka, rows, p.workgroups, s);
+}
+
+// Every expert gets the workgroups of a layer of 8 rows.
+bool launch_experts(const sa_linear::Layer& l, hipStream_t s) {
+    sa_matrix_plan p;
+    if (l.q > 4 || l.G % 128 || plan(l.q, l.N, l.K, l.G, kExpertRows, 0, &p) >= sa_matrix::kNever)
+        return false;
+    const KernelArgs ka = kernel_args(matrix_args(l), p);
+    const Rows rows = {l.epi, l.row_of, 0, l.x_rows};
+    const dim3 g((unsigned)p.workgroups * (unsigned)l.experts), b(p.threads);
+    const int n = p.workgroups;
+    switch (l.q) {
+        case 1: hipLaunchKernelGGL((k_gemm_mx_experts<1>), g, b, 0, s, ka, rows, l.offsets, l.rows, n); break;
+        case 2: hipLaunchKernelGGL((k_gemm_mx_experts<2>), g, b, 0, s, ka, rows, l.offsets, l.rows, n); break;
+        case 3: hipLaunchKernelGGL((k_gemm_mx_experts<3>), g, b, 0, s, ka, rows, l.offsets, l.rows, n); break;
+        default: hipLaunchKernelGGL((k_gemm_mx_experts<4>), g, b, 0, s, ka, rows, l.offsets, l.rows, n); break;
+    }
+    return true;
 }
 
 }  // namespace sa_mx

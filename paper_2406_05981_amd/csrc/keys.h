@@ -7,6 +7,7 @@
 #include <stdint.h>
 
 __host__ __device__ inline int imin(int a, int b) { return a < b ? a : b; }
+__host__ __device__ inline int imax(int a, int b) { return a > b ? a : b; }
 
 // Byte offset of the key of (plane i, row n, chunk c) in the packed layout.
 // Rows come in tiles of 64 and chunks in blocks of 16; a 64-row tile of one

@@ -21,6 +21,7 @@ struct Layer {
     int rows;     // rows of y
     int x_rows;   // rows of x
     int experts;  // layers
+    int few;      // experts of at most this many rows are left out
     sa_epi::Epilogue epi;
 };
 
@@ -40,10 +41,10 @@ __device__ inline bool find_tile(const Layer& a, int height, int tile, int* expe
         const int e = e0 + lane;
         int lo = 0, hi = 0;
         if (e < a.experts) {
-            lo = imin(max(a.offsets[e], 0), a.rows);
-            hi = imin(max(a.offsets[e + 1], lo), a.rows);
+            lo = imin(imax(a.offsets[e], 0), a.rows);
+            hi = imin(imax(a.offsets[e + 1], lo), a.rows);
         }
-        const int tiles = (hi - lo + height - 1) / height;
+        const int tiles = hi - lo > a.few ? (hi - lo + height - 1) / height : 0;
         int sum = tiles;
 #pragma unroll
         for (int d = 1; d < 64; d <<= 1) {
@@ -80,8 +81,29 @@ inline int64_t most_tiles(const Layer& a, int height) {
 
 }  // namespace sa_linear
 
-// Any rows, groups and planes.
+// One row of one layer, group % 128 == 0 (shiftadd.hip).
+namespace sa_rows {
+void launch(const sa_linear::Layer& a, hipStream_t s);
+}  // namespace sa_rows
+
+// 2 to 8 rows of one layer as `plan` says, and the experts of 1 to kExpertRows rows
+// (false: not this layer); up to 4 planes, group % 128 == 0 (gemm_mx.hip).
+namespace sa_mx {
+constexpr int kExpertRows = 8;
+void launch(const sa_linear::Layer& a, const sa_matrix_plan& plan, hipStream_t s);
+bool launch_experts(const sa_linear::Layer& a, hipStream_t s);
+}  // namespace sa_mx
+
+// The kernel of a few rows whose waves share the columns, one layer, up to 4 planes,
+// group % 128 == 0: estimated time (us) and call (gemm_mfma.hip).
+namespace sa_mfma {
+double plan_split(const sa_linear::Layer& a, sa_matrix_plan* plan);
+void launch(const sa_linear::Layer& a, const sa_matrix_plan& plan, hipStream_t s);
+}  // namespace sa_mfma
+
+// Any rows, groups and planes (panel.hip).
 namespace sa_panel {
+double estimate(const sa_linear::Layer& a);  // us
 void launch(const sa_linear::Layer& a, hipStream_t s);
 }  // namespace sa_panel
 

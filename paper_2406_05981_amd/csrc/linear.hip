@@ -6,6 +6,7 @@
 #include <hip/hip_runtime.h>
 
 #include "checks.h"
+#include "gemm_matrix.h"
 #include "linear.h"
 
 namespace {
@@ -30,8 +31,33 @@ int check_layer(int q, int N, int K, int group, int rows, int x_rows, int expert
 
 bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
 
-int run(const Layer& a, hipStream_t s) {
-    sa_panel::launch(a, s);
+// One layer of 2 to kFewRows rows: the kernel with the least estimated time.
+constexpr int kFewRows = 64;
+
+void run_few(const Layer& a, hipStream_t s) {
+    sa_matrix_plan mx, split;
+    const double panel = sa_panel::estimate(a);
+    const double mx_us = a.rows <= 8 ? sa_mx::plan(a.q, a.N, a.K, a.G, a.rows, 0, &mx)
+                                     : sa_matrix::kNever;
+    const double split_us = sa_mfma::plan_split(a, &split);
+    if (mx_us < split_us && mx_us < panel) sa_mx::launch(a, mx, s);
+    else if (split_us < panel) sa_mfma::launch(a, split, s);
+    else sa_panel::launch(a, s);
+}
+
+int run(Layer& a, hipStream_t s) {
+    if (a.offsets) {
+        // experts of a few rows and the others by kernels of their own, where many have few
+        if (a.rows <= sa_mx::kExpertRows * a.experts && sa_mx::launch_experts(a, s))
+            a.few = sa_mx::kExpertRows;
+        if (a.rows > a.few) sa_panel::launch(a, s);
+    } else if (a.rows == 1 && a.G % 128 == 0) {
+        sa_rows::launch(a, s);
+    } else if (a.rows <= kFewRows && a.q <= 4 && a.G % 128 == 0) {
+        run_few(a, s);
+    } else {
+        sa_panel::launch(a, s);
+    }
     return launch_status();
 }
 
@@ -49,8 +75,8 @@ SA_API int sa_shiftadd_gemm_epilogue(const uint16_t* x, const uint8_t* packed_bi
     if (!aligned16(x) || !aligned16(packed_bits) || !aligned16(y) || !aligned16(multiplier) ||
         !aligned16(residual) || !aligned4(bias))
         return SA_ERR_ALIGN;
-    const Layer a = {x, packed_bits, exps, nullptr, nullptr, q, N, K, group, rows, rows, 1,
-                     {bias, multiplier, residual, y, activation, out_half}};
+    Layer a = {x, packed_bits, exps, nullptr, nullptr, q, N, K, group, rows, rows, 1, 0,
+               {bias, multiplier, residual, y, activation, out_half}};
     return run(a, reinterpret_cast<hipStream_t>(stream));
 }
 
@@ -68,8 +94,8 @@ SA_API int sa_shiftadd_gemm_experts(const uint16_t* x, int x_rows, const int32_t
     if (!aligned16(x) || !aligned16(packed_bits) || !aligned16(y) || !aligned16(multiplier) ||
         !aligned4(bias) || !aligned4(row_of) || !aligned4(offsets))
         return SA_ERR_ALIGN;
-    const Layer a = {x, packed_bits, exps, row_of, offsets, q, N, K, group, slots, x_rows, experts,
-                     {bias, multiplier, nullptr, y, activation, out_half}};
+    Layer a = {x, packed_bits, exps, row_of, offsets, q, N, K, group, slots, x_rows, experts,
+               0, {bias, multiplier, nullptr, y, activation, out_half}};
     return run(a, reinterpret_cast<hipStream_t>(stream));
 }
 

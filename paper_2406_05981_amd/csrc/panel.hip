@@ -34,7 +34,7 @@ struct Args {
     Layer a;
     int n_tiles;           // tiles of outputs; they run fastest over the grid
     uint32_t group_magic;  // blocks to exponent groups: J * magic >> 32, 0: J
-    int vector_out;        // rows of y divide into vectors of 8
+    int byte_offsets;      // x is below 2^32 bytes
 };
 
 __device__ inline half2_t halves(uint32_t v) { return __builtin_bit_cast(half2_t, v); }
@@ -75,10 +75,17 @@ __device__ inline half2_t add_pair(const Spread& s, const Factor& f, int odd, in
     return __builtin_elementwise_fma(halves(src & (0x00010001u << pos)), m, c);
 }
 
-__device__ inline void copy_to_lds(const uint4* from, uint4* to) {
-    __builtin_amdgcn_global_load_lds(
-        (const __attribute__((address_space(1))) void*)(uintptr_t)from,
-        (__attribute__((address_space(3))) void*)to, 16, 0, 0);
+// 16 bytes a lane from memory to `lds` + 16 lane (uniform), without passing registers.
+// Written as the instruction: the compiler would make every later LDS read wait for it
+// (it does not tell the buffers apart).  There is no result in registers; whoever reads
+// the data waits for vmcnt and a barrier first.  m0 takes effect one instruction later.
+__device__ inline void copy_to_lds(uint64_t base, uint32_t offset, uint32_t lds) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
+                 :: "s"(lds), "v"(offset), "s"(base) : "m0", "memory");
+}
+__device__ inline void copy_to_lds(uint64_t from, uint32_t lds) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off"
+                 :: "s"(lds), "v"(from) : "m0", "memory");
 }
 
 __device__ inline void wave_fence() {
@@ -114,6 +121,8 @@ __device__ __forceinline__ void body(const Args& pa, uint4* xbuf) {
     constexpr int kItems = CT * 8 / RW;  // 1 KiB copies (4 rows) of a wave a block
     constexpr int kBuf = CT * 512;       // uint4 of one block
     constexpr int kE = Q > 4 ? 2 : 1;    // words of a block's exponents
+    // one row tile: two workgroups a CU (128 registers) hide more than the interleaving
+    constexpr bool kPipelined = Q <= 4 && CT > 1;
     int expert, first, end;
     if (!sa_linear::find_tile(a, kTile * CT, (int)(blockIdx.x / (unsigned)pa.n_tiles), &expert,
                               &first, &end))
@@ -133,27 +142,34 @@ __device__ __forceinline__ void body(const Args& pa, uint4* xbuf) {
     const int n0 = kTile * (RW * nt + rw);  // first output of this wave
     const int n = imin(n0 + 16 * ((r >> 2) & 1) + 4 * (r >> 3) + (r & 3), N - 1);
 
-    // rows of x that this lane copies, as 16-byte words from a.x (x is below 2^36 bytes)
+    // rows of x that this lane copies, as 16-byte words from a.x (x is below 2^36 bytes), or
+    // as bytes where these fit
     uint32_t xo[kItems];
 #pragma unroll
     for (int j = 0; j < kItems; ++j) {
         const int row = 4 * (rw * kItems + j) + (lane >> 4);
         const int v = sa_linear::source_row(a, imin(first + row, end - 1));
-        xo[j] = (uint32_t)max(v, 0) * (uint32_t)C;
+        xo[j] = (uint32_t)imax(v, 0) * (uint32_t)C;
         if constexpr (!GEN) xo[j] += (uint32_t)((lane & 15) ^ (row & 15));
+        if (pa.byte_offsets) xo[j] *= 16u;
     }
     uint4* xk = xbuf + kw * 2 * kBuf;
+    const uint32_t x_lds = (uint32_t)__builtin_amdgcn_readfirstlane(
+        (int)(uintptr_t)(__attribute__((address_space(3))) uint4*)(xk + rw * kItems * 64));
     auto copy_x = [&](int J, int buf) {
-        const uint4* base = reinterpret_cast<const uint4*>(a.x) + (GEN ? 0 : 16 * (int64_t)J);
+        const uint64_t base = (uint64_t)(uintptr_t)a.x + (GEN ? 0u : 256u * (uint64_t)J);
 #pragma unroll
         for (int j = 0; j < kItems; ++j) {
             uint32_t o = xo[j];
             asm volatile("" : "+v"(o));  // (no 64-bit pointers kept over the blocks)
             if constexpr (GEN) {
                 const int row = 4 * (rw * kItems + j) + (lane >> 4);
-                o += (uint32_t)imin(16 * J + ((lane & 15) ^ (row & 15)), C - 1);
+                const int c = imin(16 * J + ((lane & 15) ^ (row & 15)), C - 1);
+                o += (uint32_t)c * (pa.byte_offsets ? 16u : 1u);
             }
-            copy_to_lds(base + o, xk + buf * kBuf + (rw * kItems + j) * 64);
+            const uint32_t to = x_lds + 16 * (buf * kBuf + j * 64);
+            if (pa.byte_offsets) copy_to_lds(base, o, to);
+            else copy_to_lds(base + 16 * (uint64_t)o, to);
         }
     };
     // this lane's activations of step s, row tile c: word 512 c + ((2 s) ^ x_word)
@@ -219,65 +235,126 @@ __device__ __forceinline__ void body(const Args& pa, uint4* xbuf) {
         }
         return hi > 0 || lo < -14 || hi - lo > kSpread;
     };
-    // one block: w(i, h) plane i's key word of steps 4 h .. 4 h + 3, e(i, s) its exponent
-    auto summed = [&](int J, const uint4* xs, auto w, auto e) {
+    // Matrix operands of steps 2 q and 2 q + 1 of a block (q < 4): w(i, h) is plane i's key
+    // word of steps 4 h .. 4 h + 3, e(i, s) its exponent in step s.
+    auto expand = [&](int J, int q, auto w, auto e, half8_t (&W)[2]) {
+        half2_t p[2][4];
+        Factor f[2][Q];
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            half8_t W[4];
+        for (int o = 0; o < 2; ++o) {
+            half2_t sum;
 #pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                half2_t p[2][4];
-                Factor f[2][Q];
-#pragma unroll
-                for (int o = 0; o < 2; ++o) {
-                    half2_t sum;
-#pragma unroll
-                    for (int i = 0; i < Q; ++i) {
-                        const int s = 4 * h + 2 * u + o;
-                        f[o][i] = factor(e(i, s));
-                        if (Q > 4 || GEN) {
-                            const half2_t z = both(i < a.q && inside(J, s) ? 1.0f : 0.0f);
-                            f[o][i] = {f[o][i].m10 * z, f[o][i].m12 * z, f[o][i].m14 * z};
-                        }
-                        sum = i == 0 ? -f[o][i].m14 : sum - f[o][i].m14;
-                    }
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) p[o][j] = sum;
+            for (int i = 0; i < Q; ++i) {
+                f[o][i] = factor(e(i, 2 * q + o));
+                if (Q > 4 || GEN) {
+                    const half2_t z = both(i < a.q && inside(J, 2 * q + o) ? 1.0f : 0.0f);
+                    f[o][i] = {f[o][i].m10 * z, f[o][i].m12 * z, f[o][i].m14 * z};
                 }
-#pragma unroll
-                for (int i = 0; i < Q; ++i) {
-                    const Spread sp = spread(w(i, h), u);
-#pragma unroll
-                    for (int o = 0; o < 2; ++o)
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) p[o][j] = add_pair(sp, f[o][i], o, j, p[o][j]);
-                }
-                W[2 * u] = cat(p[0]);
-                W[2 * u + 1] = cat(p[1]);
-                __builtin_amdgcn_sched_barrier(0);
+                sum = i == 0 ? -f[o][i].m14 : sum - f[o][i].m14;
             }
-            // activations are read kAhead products before they are used
-            int xw = x_word;
-            asm volatile("" : "+v"(xw));  // (addresses are not kept over the blocks)
-            constexpr int kAhead = CT > 2 ? 4 : 2 * CT, kRing = kAhead + 1;
-            half8_t X[kRing];
-            auto read = [&](int q) {
-                const int s = 4 * h + q / CT, c = q % CT;
-                X[q % kRing] =
-                    __builtin_bit_cast(half8_t, xs[512 * c + ((2 * s) ^ xw)]);
-            };
 #pragma unroll
-            for (int q = 0; q < kAhead; ++q) read(q);
-            __builtin_amdgcn_sched_barrier(0);
+            for (int j = 0; j < 4; ++j) p[o][j] = sum;
+        }
 #pragma unroll
-            for (int q = 0; q < 4 * CT; ++q) {
-                if (q + kAhead < 4 * CT) read(q + kAhead);
-                acc[q % CT] = __builtin_amdgcn_mfma_f32_32x32x16_f16(W[q / CT], X[q % kRing],
-                                                                     acc[q % CT], 0, 0, 0);
-                __builtin_amdgcn_sched_barrier(0);
-            }
+        for (int i = 0; i < Q; ++i) {
+            const Spread sp = spread(w(i, q >> 1), q & 1);
+#pragma unroll
+            for (int o = 0; o < 2; ++o)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) p[o][j] = add_pair(sp, f[o][i], o, j, p[o][j]);
+        }
+        W[0] = cat(p[0]);
+        W[1] = cat(p[1]);
+    };
+    // Products of a block, activations read kAhead of them before they are used, X[i % kRing]
+    // those of product i = step * CT + row tile.
+    constexpr int kAhead = 2, kRing = kAhead + 1, kProducts = 8 * CT;
+    auto read_x = [&](const uint4* xs, int xw, int i, half8_t (&X)[kRing]) {
+        X[i % kRing] = __builtin_bit_cast(half8_t, xs[512 * (i % CT) + ((2 * (i / CT)) ^ xw)]);
+    };
+    auto products = [&](const uint4* xs, int xw, int q, const half8_t (&W)[2], half8_t (&X)[kRing]) {
+#pragma unroll
+        for (int i = 2 * CT * q; i < 2 * CT * (q + 1); ++i) {
+            if (i + kAhead < kProducts) read_x(xs, xw, i + kAhead, X);
+            acc[i % CT] = __builtin_amdgcn_mfma_f32_32x32x16_f16(W[(i / CT) & 1], X[i % kRing],
+                                                                 acc[i % CT], 0, 0, 0);
         }
     };
+    auto first_x = [&](const uint4* xs, int* xw, half8_t (&X)[kRing]) {
+        *xw = x_word;
+        asm volatile("" : "+v"(*xw));  // (addresses are not kept over the blocks)
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) read_x(xs, *xw, i, X);
+    };
+    auto summed = [&](int J, const uint4* xs, auto w, auto e) {
+        half8_t X[kRing], W[2];
+        int xw;
+        first_x(xs, &xw, X);
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            expand(J, q, w, e, W);
+            __builtin_amdgcn_sched_barrier(0);
+            products(xs, xw, q, W, X);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    };
+    // The same with the next quarter's operands expanded between one quarter's products, a
+    // piece after each: a product takes the matrix core 32 cycles, in which the two waves of
+    // a SIMD issue the expansion's vector instructions.  Pieces 0 .. Q - 1 spread a plane's
+    // word, the others are a pair each, by the position of its bits (add_pair).
+    struct Next {
+        Spread sp[Q];
+        half2_t m10[Q], m[Q];  // factors of the block for position 10, and for the position at hand
+        half2_t sum;
+        half2_t p[2][4];
+    };
+    auto new_block = [&](Next& x, auto e) {
+#pragma unroll
+        for (int i = 0; i < Q; ++i) {
+            const Factor f = factor(e(i, 0));
+            x.m10[i] = f.m10;
+            x.sum = i == 0 ? -f.m14 : x.sum - f.m14;
+        }
+    };
+    constexpr int kPieces = Q + 8;
+    auto piece = [&](Next& x, int k, int q, auto w) {
+        constexpr int kOdd[8] = {0, 1, 0, 0, 1, 0, 1, 1}, kPair[8] = {2, 1, 0, 3, 2, 1, 0, 3};
+        if (k < Q) {
+            x.sp[k] = spread(w(k, q >> 1), q & 1);
+            return;
+        }
+        const int o = kOdd[k - Q], j = kPair[k - Q];
+        if (k == Q || k == Q + 2 || k == Q + 5) {
+            const uint32_t down = k == Q ? 0u : k == Q + 2 ? 0x0C000C00u : 0x3C003C00u;
+#pragma unroll
+            for (int i = 0; i < Q; ++i)
+                x.m[i] = halves(__builtin_bit_cast(uint32_t, x.m10[i]) - down);
+        }
+        half2_t c = x.sum;
+#pragma unroll
+        for (int i = 0; i < Q; ++i) c = add_pair(x.sp[i], {x.m[i], x.m[i], x.m[i]}, o, j, c);
+        x.p[o][j] = c;
+    };
+    auto take = [&](const Next& x, half8_t (&W)[2]) {
+        W[0] = cat(x.p[0]);
+        W[1] = cat(x.p[1]);
+    };
+    auto quarter = [&](const uint4* xs, int xw, int q, const half8_t (&W)[2], half8_t (&X)[kRing],
+                       auto next) {
+        constexpr int n = 2 * CT;
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int u = 0; u < n; ++u) {
+            const int i = n * q + u;
+            if (i + kAhead < kProducts) read_x(xs, xw, i + kAhead, X);
+            acc[i % CT] = __builtin_amdgcn_mfma_f32_32x32x16_f16(W[(i / CT) & 1], X[i % kRing],
+                                                                 acc[i % CT], 0, 0, 0);
+#pragma unroll
+            for (int k = (u * kPieces + n - 1) / n; k < ((u + 1) * kPieces + n - 1) / n; ++k) next(k);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    };
+
     // Any exponents: a product a plane in bfloat16, whose range holds +-2^e, with the
     // activations as two exact pieces.
     auto plane_by_plane = [&](int J, const uint4* xs, auto w, auto e) {
@@ -413,19 +490,57 @@ __device__ __forceinline__ void body(const Args& pa, uint4* xbuf) {
             uint32_t wd[2][Q][2], ew[2][kE];
             const bool far = __any(unpack(k, wd, ew) && blk0 + s0 + g < blk1);
             left |= far;
-            auto step = [&](auto bc) {
-                constexpr int b = decltype(bc)::value;
-                const int J = blk0 + s0 + b;
-                if (s0 + b >= steps) return;
-                if (J + 1 < blk1) copy_x(J + 1, (b + 1) & 1);
-                if (b == 1 && J + 1 < blk1) load_keys(J + 1, k);
-                if (J < blk1 && !far)
-                    summed(J, xr + b * kBuf, [&](int i, int h) { return wd[b][i][h]; },
-                           [&](int i, int) { return (int)(int8_t)(ew[b][i >> 2] >> (8 * (i & 3))); });
-                arrive();
-            };
-            step(std::integral_constant<int, 0>{});
-            step(std::integral_constant<int, 1>{});
+            const int J0 = blk0 + s0;
+            auto e0 = [&](int i, int) { return (int)(int8_t)(ew[0][i >> 2] >> (8 * (i & 3))); };
+            auto e1 = [&](int i, int) { return (int)(int8_t)(ew[1][i >> 2] >> (8 * (i & 3))); };
+            auto w0 = [&](int i, int h) { return wd[0][i][h]; };
+            auto w1 = [&](int i, int h) { return wd[1][i][h]; };
+            const bool run = J0 < blk1 && !far;
+            if (J0 + 1 < blk1) copy_x(J0 + 1, 1);
+            half8_t W[2], X[kRing];
+            Next x;
+            int xw;
+            if constexpr (kPipelined) {
+                if (run) {
+                    first_x(xr, &xw, X);
+                    new_block(x, e0);
+#pragma unroll
+                    for (int u = 0; u < kPieces; ++u) piece(x, u, 0, w0);
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        take(x, W);
+                        if (q == 3) new_block(x, e1);  // (unused if there is no second block)
+                        quarter(xr, xw, q, W, X, [&](int u) {
+                            if (q < 3) piece(x, u, q + 1, w0);
+                            else piece(x, u, 0, w1);
+                        });
+                    }
+                }
+            } else if (run) {
+                summed(J0, xr, w0, e0);
+            }
+            arrive();
+            if (s0 + 1 >= steps) break;
+            if (J0 + 2 < blk1) {
+                copy_x(J0 + 2, 0);
+                load_keys(J0 + 2, k);
+            }
+            const uint4* xs = xr + kBuf;
+            if (run && J0 + 1 < blk1) {
+                if constexpr (kPipelined) {
+                    first_x(xs, &xw, X);
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        take(x, W);
+                        quarter(xs, xw, q, W, X, [&](int u) {
+                            if (q < 3) piece(x, u, q + 1, w1);
+                        });
+                    }
+                } else {
+                    summed(J0 + 1, xs, w1, e1);
+                }
+            }
+            arrive();
         }
     }
     // the second loop runs the groups that the first one left, the same in every way
@@ -445,13 +560,18 @@ __device__ __forceinline__ void body(const Args& pa, uint4* xbuf) {
                     uint32_t wd[2][Q][2], ew[2][kE];
                     load_keys(J & ~1, k);
                     if (__any(unpack(k, wd, ew) && (J & ~1) + g < blk1)) {
-                        const bool b = J & 1;
-                        plane_by_plane(J, xr,
-                                       [&](int i, int h) { return b ? wd[1][i][h] : wd[0][i][h]; },
-                                       [&](int i, int) {
-                                           const uint32_t ei = b ? ew[1][i >> 2] : ew[0][i >> 2];
-                                           return (int)(int8_t)(ei >> (8 * (i & 3)));
-                                       });
+                        // block J & 1, by selects (values the compiler cannot turn into an
+                        // indexed array in memory)
+                        auto pick = [&](uint32_t w0, uint32_t w1) {
+                            asm volatile("" : "+v"(w0), "+v"(w1));
+                            return J & 1 ? w1 : w0;
+                        };
+                        plane_by_plane(
+                            J, xr, [&](int i, int h) { return pick(wd[0][i][h], wd[1][i][h]); },
+                            [&](int i, int) {
+                                const uint32_t e = pick(ew[0][i >> 2], ew[1][i >> 2]);
+                                return (int)(int8_t)(e >> (8 * (i & 3)));
+                            });
                     }
                 }
             }
@@ -467,8 +587,15 @@ __device__ __forceinline__ void body(const Args& pa, uint4* xbuf) {
     static_assert(CT % kPasses == 0 && kWaves * kVals <= KW * 2 * kBuf * 4, "sums fit the buffers");
     float* red = reinterpret_cast<float*>(xbuf) + lane;
     const int nb = n0 + 16 * g;
-    sa_epi::Epilogue epi = a.epi;
-    if (epi.bias) epi.bias += (int64_t)expert * N;
+    const sa_epi::Epilogue& epi = a.epi;
+    // (KW > 1: a wave's vectors are all first or all second halves of the 16)
+    constexpr int kHalves = KW > 1 ? 1 : 2;
+    float bias[kHalves][8];
+#pragma unroll
+    for (int j = 0; j < 8 * kHalves; ++j) {
+        const int nn = nb + (KW > 1 ? 8 * (kw & 1) : 0) + j;
+        bias[j >> 3][j & 7] = epi.bias ? epi.bias[(int64_t)expert * N + imin(nn, N - 1)] : 0.0f;
+    }
 #pragma unroll
     for (int pass = 0; pass < kPasses; ++pass) {
 #pragma unroll
@@ -478,29 +605,46 @@ __device__ __forceinline__ void body(const Args& pa, uint4* xbuf) {
                 red[wave * kVals + (c * 16 + v) * 64] = acc[pass * kPass + c][v];
         if constexpr (KW > 1) __syncthreads();
         else wave_fence();
+        // kUnroll vectors of 8 outputs at a time, their operands requested together
+        constexpr int kVectors = (2 * kPass + KW - 1) / KW, kUnroll = kVectors < 4 ? kVectors : 4;
 #pragma unroll 1
-        for (int o = KW > 1 ? kw : 0; o < 2 * kPass; o += KW) {
-            const int c = o >> 1, nn = nb + 8 * (o & 1);
-            const int row = first + kTile * (pass * kPass + c) + r;
-            if (row >= end || nn >= N || sa_linear::source_row(a, row) < 0) continue;
-            float v[8];
+        for (int o0 = KW > 1 ? kw : 0; o0 < 2 * kPass; o0 += kUnroll * KW) {
+            sa_epi::Operands8 operands[kUnroll];
+            int64_t at[kUnroll];
+            int count[kUnroll];  // outputs of the vector, at most 0: none
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const float* p = red + rw * kVals + (o * 8 + j) * 64;
-                v[j] = p[0];
-#pragma unroll
-                for (int u = 1; u < KW; ++u) v[j] += p[u * RW * kVals];
+            for (int u = 0; u < kUnroll; ++u) {
+                const int o = o0 + u * KW, nn = nb + 8 * (o & 1);
+                const int row = first + kTile * (pass * kPass + (o >> 1)) + r;
+                at[u] = (int64_t)row * N + nn;
+                count[u] = o < 2 * kPass && row < end && sa_linear::source_row(a, row) >= 0
+                               ? N - nn
+                               : 0;
+                if (count[u] >= 8) sa_epi::fetch(epi, at[u], &operands[u]);
             }
-            const int64_t at = (int64_t)row * N + nn;
-            if (pa.vector_out) sa_epi::finish_vector<8>(epi, at, nn, v);
-            else sa_epi::finish_some<8>(epi, at, nn, N - nn, v);
+#pragma unroll
+            for (int u = 0; u < kUnroll; ++u) {
+                if (count[u] < 1) continue;
+                const int o = o0 + u * KW;
+                float v[8];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const float* p = red + rw * kVals + (o * 8 + j) * 64;
+                    v[j] = p[0];
+#pragma unroll
+                    for (int x = 1; x < KW; ++x) v[j] += p[x * RW * kVals];
+                }
+                if (count[u] >= 8) sa_epi::finish(epi, at[u], bias[u % kHalves], operands[u], v);
+                else sa_epi::finish_some(epi, at[u], bias[u % kHalves], count[u], v);
+            }
         }
         if constexpr (kPasses > 1) wave_fence();
     }
 }
 
 template <int Q, int CT, int KW, bool GEN>
-__global__ __launch_bounds__(kThreads, 2) void k_panel(Args pa) {
+__global__ __launch_bounds__(kThreads, CT == 1 && Q <= 4 && !GEN ? 4 : 2)
+void k_panel(Args pa) {
     __shared__ uint4 xbuf[KW * 2 * CT * 512];
     body<Q, CT, KW, GEN>(pa, xbuf);
 }
@@ -509,42 +653,102 @@ template <int Q, int CT, int KW, bool GEN>
 void start(Args& pa, hipStream_t s) {
     const int cols = kTile * (kWaves / KW);
     pa.n_tiles = (pa.a.N + cols - 1) / cols;
-    pa.vector_out = pa.a.N % 8 == 0;
     const int64_t tiles = sa_linear::most_tiles(pa.a, kTile * CT);
     hipLaunchKernelGGL((k_panel<Q, CT, KW, GEN>), dim3((unsigned)(tiles * pa.n_tiles)),
                        dim3(kThreads), 0, s, pa);
 }
 
-template <int Q>
-void start_tiles(Args& pa, int ct, hipStream_t s) {
-    if (ct == 8) start<Q, 8, 1, false>(pa, s);
-    else if (ct == 4) start<Q, 4, 1, false>(pa, s);
-    else if (ct == 2) start<Q, 2, 2, false>(pa, s);
-    else start<Q, 1, 4, false>(pa, s);
+// Tiles of a workgroup: 32 ct rows and 256 / kw outputs.  The estimates (us) are fitted
+// to every form's time on 590 drawn layers of N 64..28672, K 128..28672, q 1..4, 2..8192
+// rows, weights rotated over 320 MB (5th and 95th percentile of estimate / measured 0.7
+// and 1.4): a base; a workgroup alone, per 128-column block of a share a fixed part and
+// one per plane, and an end; rounds of workgroups over the CUs, the same.  The form of
+// least estimate takes 1.012 times the best form's time in the mean, 1.14 at the 99th
+// percentile.  More than 4 planes (registers) and groups that are not multiples of 128
+// have the forms of one and two row tiles, or four.
+struct Form {
+    int ct, kw;
+    double base, alone, alone_q, shared, shared_q, end;
+};
+constexpr Form kForms[] = {{8, 1, 3.8, 1.86, 0.38, 5.6, 0.17, 20.0},
+                           {4, 1, 0.0, 0.88, 0.39, 2.6, 0.30, 9.7},
+                           {4, 2, 0.0, 1.07, 0.37, 2.2, 0.36, 6.8},
+                           {2, 2, 0.0, 0.56, 0.41, 0.68, 0.49, 5.3},
+                           {2, 4, 0.0, 0.74, 0.43, 1.04, 0.41, 4.5},
+                           {1, 4, 2.4, 0.36, 0.47, 0.35, 0.43, 1.5},
+                           {1, 8, 0.9, 0.68, 0.40, 0.80, 0.44, 2.8}};
+
+// (blocks to groups by multiplication: up to 2^22 columns)
+bool general(const Layer& a) { return a.G % 128 || a.K > (1 << 22); }
+
+double choose(const Layer& a, const Form** best) {
+    const int blocks = (a.K + 127) / 128;
+    // rows of an expert, as if all had the same
+    const int64_t per = a.offsets ? (a.rows + a.experts - 1) / a.experts : a.rows;
+    double least = 1e30;
+    for (const Form& f : kForms) {
+        if (f.ct > (a.q > 4 ? 2 : general(a) ? 4 : 8)) continue;
+        const int64_t tall = (per + 32 * f.ct - 1) / (32 * f.ct) *
+                             (a.offsets ? imin(a.experts, a.rows) : 1);
+        const double r = (double)(tall * ((a.N + 256 / f.kw - 1) / (256 / f.kw))) / 256;
+        const double rounds = r <= 1 ? r : 0.5 * (r + (double)(int64_t)(r + 0.999999));
+        const int steps = imin(2 * (((blocks + 1) / 2 + f.kw - 1) / f.kw), blocks);
+        const double alone = steps * (f.alone + f.alone_q * a.q) + f.end;
+        const double shared = rounds * (steps * (f.shared + f.shared_q * a.q) + f.end);
+        const double us = f.base + (alone > shared ? alone : shared);
+        if (us < least) {
+            least = us;
+            *best = &f;
+        }
+    }
+    return least;
+}
+
+template <int Q, bool GEN>
+void start_form(Args& pa, const Form& f, hipStream_t s) {
+    switch (10 * f.ct + f.kw) {
+        case 81:
+            if constexpr (Q <= 4 && !GEN) start<Q, 8, 1, GEN>(pa, s);
+            break;
+        case 41:
+            if constexpr (Q <= 4) start<Q, 4, 1, GEN>(pa, s);
+            break;
+        case 42:
+            if constexpr (Q <= 4) start<Q, 4, 2, GEN>(pa, s);
+            break;
+        case 22: start<Q, 2, 2, GEN>(pa, s); break;
+        case 24: start<Q, 2, 4, GEN>(pa, s); break;
+        case 14: start<Q, 1, 4, GEN>(pa, s); break;
+        default: start<Q, 1, 8, GEN>(pa, s); break;
+    }
 }
 
 }  // namespace
+
+double estimate(const Layer& a) {
+    const Form* f;
+    return choose(a, &f);
+}
 
 void launch(const Layer& a, hipStream_t s) {
     Args pa{};
     pa.a = a;
     const uint32_t d = (uint32_t)(a.G / 128);
     pa.group_magic = d <= 1 ? 0u : (uint32_t)(((1ull << 32) + d - 1) / d);
-    const int per = a.offsets ? (a.rows + a.experts - 1) / a.experts : a.rows;
-    const int ct = per > 512 ? 8 : per > 128 ? 4 : per > 32 ? 2 : 1;
-    // blocks to groups by multiplication: up to 2^22 columns
-    if (a.G % 128 || a.K > (1 << 22)) {
-        if (a.q > 4) start<8, 1, 4, true>(pa, s);
-        else if (ct >= 4) start<4, 4, 1, true>(pa, s);
-        else start<4, 1, 4, true>(pa, s);
+    pa.byte_offsets = (int64_t)a.x_rows * a.K < (int64_t)1 << 31;
+    const Form* f;
+    choose(a, &f);
+    if (general(a)) {
+        if (a.q > 4) start_form<8, true>(pa, *f, s);
+        else start_form<4, true>(pa, *f, s);
         return;
     }
     switch (a.q) {
-        case 1: start_tiles<1>(pa, ct, s); break;
-        case 2: start_tiles<2>(pa, ct, s); break;
-        case 3: start_tiles<3>(pa, ct, s); break;
-        case 4: start_tiles<4>(pa, ct, s); break;
-        default: start<8, 2, 2, false>(pa, s); break;
+        case 1: start_form<1, false>(pa, *f, s); break;
+        case 2: start_form<2, false>(pa, *f, s); break;
+        case 3: start_form<3, false>(pa, *f, s); break;
+        case 4: start_form<4, false>(pa, *f, s); break;
+        default: start_form<8, false>(pa, *f, s); break;
     }
 }
 

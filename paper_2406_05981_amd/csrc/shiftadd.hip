@@ -13,6 +13,7 @@
 #include "checks.h"
 #include "gemm_matrix.h"
 #include "keys.h"
+#include "linear.h"
 #include "shiftadd.h"
 
 #define SA_VERSION_STRING "0.1.0 gfx950"
@@ -243,7 +244,11 @@ struct RowsArgs {
     int row_block, NB;  // block-wise: rows per block, blocks
     const int8_t* term_signs;  // additive: [q][N][K/G][T], with exps [q][N][K/G][T]
     int terms;                 // additive: T
+    sa_epi::Epilogue epi;      // kEpilogue: what follows the sum (one batch row)
 };
+
+// What an output is: fp32, binary16, or the epilogue of the sum.
+enum Output { kFp32 = 0, kHalf = 1, kEpilogue = 2 };
 
 // Where the power-of-two factors sit: one per (plane, row, group of G columns),
 // one per (plane, column), one per (plane, block of rows, 8-column key), or a
@@ -476,8 +481,8 @@ __device__ inline float job_sum(JobRegs<Q>& j, uint32_t rgn_lo, uint32_t rgn_hi,
 // H = 2 (layers of several pieces with at most one workgroup per CU): 16
 // waves, the second 8 taking the odd pieces with their own 64 KB of tables, so
 // two pieces are in flight per CU; the 16 waves' row sums meet at the end.
-// OUT16: y holds binary16 outputs (row-wise layer only).
-template <int Q, int U, int MODE, int H = 1, bool OUT16 = false>
+// OUT: kHalf and kEpilogue with the row-wise layer only, kEpilogue at one batch row.
+template <int Q, int U, int MODE, int H = 1, int OUT = kFp32>
 __device__ __forceinline__ void gemm_rows_body(const RowsArgs& a, float* lut,
                                                float (*red)[kGroupRows * kMaxRG]) {
     constexpr bool COL = MODE == kColWise;
@@ -497,6 +502,14 @@ __device__ __forceinline__ void gemm_rows_body(const RowsArgs& a, float* lut,
     const int pieces = (pieces_all - half + H - 1) / H;  // this half's pieces
     const int planes = COL ? a.q : 1;
     const int jobs = a.B * planes * pieces * nrg;
+
+    // a thread has one output at most: its operands are requested first
+    static_assert(kGroupRows * kMaxRG <= kRowThreads, "one output a thread");
+    sa_epi::Operands operands{};
+    if constexpr (OUT == kEpilogue) {
+        const int n = kGroupRows * rg0 + (int)threadIdx.x;
+        if ((int)threadIdx.x < kGroupRows * nrg && n < a.N) operands = sa_epi::fetch(a.epi, n, n);
+    }
 
     // LDS address parts of this lane's 16 key positions, two positions per
     // register: bytes 0 and 1 of offs[k] are 4*slot of positions 2k and
@@ -629,7 +642,10 @@ __device__ __forceinline__ void gemm_rows_body(const RowsArgs& a, float* lut,
                     float s = red[0][t];
 #pragma unroll
                     for (int w = 1; w < kRowWaves * H; ++w) s += red[w][t];
-                    store_out(a.y, (int64_t)j.b * a.N + n, s, OUT16);
+                    if constexpr (OUT == kEpilogue)
+                        sa_epi::finish(a.epi, n, operands, s);
+                    else
+                        store_out(a.y, (int64_t)j.b * a.N + n, s, OUT);
                 }
             }
             // red is rewritten by the next batch row
@@ -705,19 +721,19 @@ constexpr int rows_jobs_per_iter() { return 1; }
 
 // Up to 4 planes: two 8-wave workgroups per CU (4 waves per SIMD, <= 128
 // VGPRs).  More planes need more registers: one workgroup per CU.
-template <int Q, int H = 1, bool OUT16 = false>
+template <int Q, int H = 1, int OUT = kFp32>
 __global__ __launch_bounds__(kRowThreads * H) __attribute__((amdgpu_waves_per_eu(4)))
 void k_gemm_rows(RowsArgs a) {
     __shared__ float lut[H * 16 * kRegionFloats];  // 64 KB per half
     __shared__ float red[kRowWaves * H][kGroupRows * kMaxRG];
-    gemm_rows_body<Q, rows_jobs_per_iter<Q>(), kRowWise, H, OUT16>(a, lut, red);
+    gemm_rows_body<Q, rows_jobs_per_iter<Q>(), kRowWise, H, OUT>(a, lut, red);
 }
 
-template <int Q, bool OUT16 = false>
+template <int Q, int OUT = kFp32>
 __global__ __launch_bounds__(kRowThreads) void k_gemm_rows_wide(RowsArgs a) {
     __shared__ float lut[16 * kRegionFloats];  // 64 KB
     __shared__ float red[kRowWaves][kGroupRows * kMaxRG];
-    gemm_rows_body<Q, rows_jobs_per_iter<Q>(), kRowWise, 1, OUT16>(a, lut, red);
+    gemm_rows_body<Q, rows_jobs_per_iter<Q>(), kRowWise, 1, OUT>(a, lut, red);
 }
 
 // Column-wise factors: one plane per job, registers of a one-plane job.
@@ -1569,27 +1585,27 @@ int grid_for(int64_t items) {
     return (int)g;
 }
 
-template <bool OUT16 = false>
+template <int OUT = kFp32>
 void launch_rows(int q, const RowsArgs& a, int workgroups, int split, hipStream_t s) {
     const dim3 g(workgroups), b(kRowThreads * split);
     if (split == 2) {
         switch (q) {
-            case 1: hipLaunchKernelGGL((k_gemm_rows<1, 2, OUT16>), g, b, 0, s, a); break;
-            case 2: hipLaunchKernelGGL((k_gemm_rows<2, 2, OUT16>), g, b, 0, s, a); break;
-            case 3: hipLaunchKernelGGL((k_gemm_rows<3, 2, OUT16>), g, b, 0, s, a); break;
-            default: hipLaunchKernelGGL((k_gemm_rows<4, 2, OUT16>), g, b, 0, s, a); break;
+            case 1: hipLaunchKernelGGL((k_gemm_rows<1, 2, OUT>), g, b, 0, s, a); break;
+            case 2: hipLaunchKernelGGL((k_gemm_rows<2, 2, OUT>), g, b, 0, s, a); break;
+            case 3: hipLaunchKernelGGL((k_gemm_rows<3, 2, OUT>), g, b, 0, s, a); break;
+            default: hipLaunchKernelGGL((k_gemm_rows<4, 2, OUT>), g, b, 0, s, a); break;
         }
         return;
     }
     switch (q) {
-        case 1: hipLaunchKernelGGL((k_gemm_rows<1, 1, OUT16>), g, b, 0, s, a); break;
-        case 2: hipLaunchKernelGGL((k_gemm_rows<2, 1, OUT16>), g, b, 0, s, a); break;
-        case 3: hipLaunchKernelGGL((k_gemm_rows<3, 1, OUT16>), g, b, 0, s, a); break;
-        case 4: hipLaunchKernelGGL((k_gemm_rows<4, 1, OUT16>), g, b, 0, s, a); break;
-        case 5: hipLaunchKernelGGL((k_gemm_rows_wide<5, OUT16>), g, b, 0, s, a); break;
-        case 6: hipLaunchKernelGGL((k_gemm_rows_wide<6, OUT16>), g, b, 0, s, a); break;
-        case 7: hipLaunchKernelGGL((k_gemm_rows_wide<7, OUT16>), g, b, 0, s, a); break;
-        default: hipLaunchKernelGGL((k_gemm_rows_wide<8, OUT16>), g, b, 0, s, a); break;
+        case 1: hipLaunchKernelGGL((k_gemm_rows<1, 1, OUT>), g, b, 0, s, a); break;
+        case 2: hipLaunchKernelGGL((k_gemm_rows<2, 1, OUT>), g, b, 0, s, a); break;
+        case 3: hipLaunchKernelGGL((k_gemm_rows<3, 1, OUT>), g, b, 0, s, a); break;
+        case 4: hipLaunchKernelGGL((k_gemm_rows<4, 1, OUT>), g, b, 0, s, a); break;
+        case 5: hipLaunchKernelGGL((k_gemm_rows_wide<5, OUT>), g, b, 0, s, a); break;
+        case 6: hipLaunchKernelGGL((k_gemm_rows_wide<6, OUT>), g, b, 0, s, a); break;
+        case 7: hipLaunchKernelGGL((k_gemm_rows_wide<7, OUT>), g, b, 0, s, a); break;
+        default: hipLaunchKernelGGL((k_gemm_rows_wide<8, OUT>), g, b, 0, s, a); break;
     }
 }
 
@@ -1647,6 +1663,24 @@ void launch_batch_pre(int q, int kw, const BatchArgs& a, int workgroups, hipStre
 }
 
 }  // namespace
+
+// One row with its epilogue, group % 128 == 0.
+void sa_rows::launch(const sa_linear::Layer& l, hipStream_t s) {
+    sa_plan plan;
+    make_plan(l.q, l.N, l.K, l.G, 1, &plan);
+    RowsArgs a{};
+    a.x = l.x;
+    a.packed = l.packed;
+    a.exps = l.exps;
+    a.q = l.q;
+    a.N = l.N;
+    a.K = l.K;
+    a.G = l.G;
+    a.B = 1;
+    a.groups = (l.N + kGroupRows - 1) / kGroupRows;
+    a.epi = l.epi;
+    launch_rows<kEpilogue>(l.q, a, plan.workgroups, plan.threads / kRowThreads, s);
+}
 
 extern "C" {
 
@@ -1770,7 +1804,7 @@ int shiftadd_gemm(const uint16_t* x, const uint8_t* packed_bits, const int8_t* e
     a.y = y;
     a.groups = (N + kGroupRows - 1) / kGroupRows;
     if (out_half)
-        launch_rows<true>(q, a, plan.workgroups, plan.threads / kRowThreads, s);
+        launch_rows<kHalf>(q, a, plan.workgroups, plan.threads / kRowThreads, s);
     else
         launch_rows(q, a, plan.workgroups, plan.threads / kRowThreads, s);
     return launch_status();

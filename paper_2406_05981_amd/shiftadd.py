@@ -9,6 +9,7 @@ raises :class:`SaError` with the library's status text.
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 from typing import Optional
 
@@ -136,15 +137,15 @@ def _stream(stream) -> int:
 def _dev(t: torch.Tensor, name: str, dtype: torch.dtype, numel: int) -> int:
     if not isinstance(t, torch.Tensor):
         raise TypeError(f"{name} must be a torch.Tensor")
+    if t.dtype == dtype and t.is_cuda and t.numel() == numel and t.is_contiguous():
+        return t.data_ptr()
     if not t.is_cuda:
         raise ValueError(f"{name} must be on the GPU")
     if t.dtype != dtype:
         raise ValueError(f"{name} must be {dtype}, got {t.dtype}")
     if not t.is_contiguous():
         raise ValueError(f"{name} must be contiguous")
-    if t.numel() != numel:
-        raise ValueError(f"{name} must have {numel} elements, got {t.numel()}")
-    return t.data_ptr()
+    raise ValueError(f"{name} must have {numel} elements, got {t.numel()}")
 
 
 def _opt(t: Optional[torch.Tensor], name: str, dtype: torch.dtype, numel: int) -> Optional[int]:
@@ -152,9 +153,21 @@ def _opt(t: Optional[torch.Tensor], name: str, dtype: torch.dtype, numel: int) -
 
 
 def _activation(name: str) -> int:
-    if name not in ACTIVATIONS:
+    act = ACTIVATIONS.get(name)
+    if act is None:
         raise ValueError(f"activation must be one of {', '.join(ACTIVATIONS)}, got {name!r}")
-    return ACTIVATIONS[name]
+    return act
+
+
+# A layer of a few us waits for its call: sizes are checked once a layer shape.
+@functools.lru_cache(maxsize=1024)
+def _layer_bytes(q: int, N: int, K: int, group: int, where: str) -> int:
+    nbytes = sa_packed_bytes(q, N, K)
+    if nbytes == 0:
+        _check(SA_ERR_SHAPE if 1 <= q <= SA_MAX_Q else SA_ERR_Q, where)
+    if group <= 0 or K % group:
+        _check(SA_ERR_GROUP, where)
+    return nbytes
 
 
 def _out_half(y: torch.Tensor) -> int:
@@ -333,19 +346,20 @@ def sa_shiftadd_gemm_epilogue(x: torch.Tensor, packed_bits: torch.Tensor, exps: 
                               stream=None) -> None:
     """``y = activation(x W_q^T + bias) * multiplier + residual``; fp32 or binary16 by
     ``y``'s type, which ``multiplier`` and ``residual`` share."""
-    if sa_packed_bytes(q, N, K) == 0:
-        _check(SA_ERR_SHAPE if 1 <= q <= SA_MAX_Q else SA_ERR_Q, "sa_shiftadd_gemm_epilogue")
-    if group <= 0 or K % group:
-        _check(SA_ERR_GROUP, "sa_shiftadd_gemm_epilogue")
+    nbytes = _layer_bytes(q, N, K, group, "sa_shiftadd_gemm_epilogue")
     half = _out_half(y)
-    _check(lib.sa_shiftadd_gemm_epilogue(
+    dtype, n = y.dtype, rows * N
+    status = lib.sa_shiftadd_gemm_epilogue(
         _dev(x, "x", torch.float16, rows * K),
-        _dev(packed_bits, "packed_bits", torch.uint8, sa_packed_bytes(q, N, K)),
+        _dev(packed_bits, "packed_bits", torch.uint8, nbytes),
         _dev(exps, "exps", torch.int8, q * N * (K // group)),
-        q, N, K, group, rows, _opt(bias, "bias", torch.float32, N), _activation(activation),
-        _opt(multiplier, "multiplier", y.dtype, rows * N),
-        _opt(residual, "residual", y.dtype, rows * N),
-        half, _dev(y, "y", y.dtype, rows * N), _stream(stream)), "sa_shiftadd_gemm_epilogue")
+        q, N, K, group, rows,
+        None if bias is None else _dev(bias, "bias", torch.float32, N), _activation(activation),
+        None if multiplier is None else _dev(multiplier, "multiplier", dtype, n),
+        None if residual is None else _dev(residual, "residual", dtype, n),
+        half, _dev(y, "y", dtype, n), _stream(stream))
+    if status != SA_OK:
+        _check(status, "sa_shiftadd_gemm_epilogue")
 
 
 def sa_shiftadd_gemm_experts(x: torch.Tensor, row_of: Optional[torch.Tensor],
@@ -356,17 +370,14 @@ def sa_shiftadd_gemm_experts(x: torch.Tensor, row_of: Optional[torch.Tensor],
                              y: torch.Tensor, stream=None) -> None:
     """``y[s] = activation(x[row_of[s]] W_q^e^T + bias[e]) * multiplier[s]`` for the slots
     ``offsets[e] <= s < offsets[e + 1]`` of every expert e."""
-    if sa_packed_bytes(q, N, K) == 0:
-        _check(SA_ERR_SHAPE if 1 <= q <= SA_MAX_Q else SA_ERR_Q, "sa_shiftadd_gemm_experts")
-    if group <= 0 or K % group:
-        _check(SA_ERR_GROUP, "sa_shiftadd_gemm_experts")
+    nbytes = _layer_bytes(q, N, K, group, "sa_shiftadd_gemm_experts")
     half = _out_half(y)
     x_rows = x.numel() // K if isinstance(x, torch.Tensor) else 0
     _check(lib.sa_shiftadd_gemm_experts(
         _dev(x, "x", torch.float16, x_rows * K), x_rows,
         _opt(row_of, "row_of", torch.int32, slots),
         _dev(offsets, "offsets", torch.int32, experts + 1),
-        _dev(packed_bits, "packed_bits", torch.uint8, experts * sa_packed_bytes(q, N, K)),
+        _dev(packed_bits, "packed_bits", torch.uint8, experts * nbytes),
         _dev(exps, "exps", torch.int8, experts * q * N * (K // group)),
         q, N, K, group, experts, slots, _opt(bias, "bias", torch.float32, experts * N),
         _activation(activation), _opt(multiplier, "multiplier", y.dtype, slots * N),
