@@ -25,8 +25,9 @@ struct Layer {
     sa_epi::Epilogue epi;
 };
 
-// The `tile`-th tile of `height` rows, counted over the experts' rows: its expert and
-// rows [first, end).  Every lane of a wave calls it; false past the last tile.
+// The `tile`-th tile of `height` rows, counted over the experts' rows, whole tiles of all
+// experts before the shorter ones at their ends: its expert and rows [first, end).  Every
+// lane of a wave calls it; false past the last tile.
 __device__ inline bool find_tile(const Layer& a, int height, int tile, int* expert, int* first,
                                  int* end) {
     if (!a.offsets) {
@@ -36,32 +37,35 @@ __device__ inline bool find_tile(const Layer& a, int height, int tile, int* expe
         return *first < a.rows;
     }
     const int lane = threadIdx.x & 63;
-    int before = 0;  // tiles of the experts below e0
-    for (int e0 = 0; e0 < a.experts; e0 += 64) {
-        const int e = e0 + lane;
-        int lo = 0, hi = 0;
-        if (e < a.experts) {
-            lo = imin(imax(a.offsets[e], 0), a.rows);
-            hi = imin(imax(a.offsets[e + 1], lo), a.rows);
-        }
-        const int tiles = hi - lo > a.few ? (hi - lo + height - 1) / height : 0;
-        int sum = tiles;
+    int before = 0;  // tiles counted
+    for (int whole = 1; whole >= 0; --whole)
+        for (int e0 = 0; e0 < a.experts; e0 += 64) {
+            const int e = e0 + lane;
+            int lo = 0, hi = 0;
+            if (e < a.experts) {
+                lo = imin(imax(a.offsets[e], 0), a.rows);
+                hi = imin(imax(a.offsets[e + 1], lo), a.rows);
+            }
+            const int rows = hi - lo > a.few ? hi - lo : 0;
+            const int tiles = whole ? rows / height : (int)(rows % height != 0);
+            if (!whole) lo += rows / height * height;
+            int sum = tiles;
 #pragma unroll
-        for (int d = 1; d < 64; d <<= 1) {
-            const int v = __shfl_up(sum, d);
-            if (lane >= d) sum += v;
+            for (int d = 1; d < 64; d <<= 1) {
+                const int v = __shfl_up(sum, d);
+                if (lane >= d) sum += v;
+            }
+            const int total = __shfl(sum, 63);
+            if (tile < before + total) {
+                const int l = __builtin_ctzll(__ballot(tile < before + sum));
+                const int f = __shfl(lo, l) + height * (tile - before - __shfl(sum - tiles, l));
+                *expert = __builtin_amdgcn_readfirstlane(e0 + l);
+                *first = __builtin_amdgcn_readfirstlane(f);
+                *end = __builtin_amdgcn_readfirstlane(__shfl(hi, l));
+                return true;
+            }
+            before += total;
         }
-        const int total = __shfl(sum, 63);
-        if (tile < before + total) {
-            const int l = __builtin_ctzll(__ballot(tile < before + sum));
-            const int f = __shfl(lo, l) + height * (tile - before - __shfl(sum - tiles, l));
-            *expert = __builtin_amdgcn_readfirstlane(e0 + l);
-            *first = __builtin_amdgcn_readfirstlane(f);
-            *end = __builtin_amdgcn_readfirstlane(__shfl(hi, l));
-            return true;
-        }
-        before += total;
-    }
     return false;
 }
 

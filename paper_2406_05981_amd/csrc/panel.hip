@@ -115,7 +115,7 @@ struct Keys {
 // a block are 256 bytes of LDS, chunk c at 16 (c ^ (row & 15)): both the copies (whole
 // rows) and the reads (16 lanes at a time, one step) touch every bank once.
 template <int Q, int CT, int KW, bool GEN>
-__device__ __forceinline__ void body(const Args& pa, uint4* xbuf) {
+__device__ __forceinline__ void body(const Args& pa, uint4* xbuf, int expert, int first, int end) {
     const Layer& a = pa.a;
     constexpr int RW = kWaves / KW;
     constexpr int kItems = CT * 8 / RW;  // 1 KiB copies (4 rows) of a wave a block
@@ -123,10 +123,6 @@ __device__ __forceinline__ void body(const Args& pa, uint4* xbuf) {
     constexpr int kE = Q > 4 ? 2 : 1;    // words of a block's exponents
     // one row tile: two workgroups a CU (128 registers) hide more than the interleaving
     constexpr bool kPipelined = Q <= 4 && CT > 1;
-    int expert, first, end;
-    if (!sa_linear::find_tile(a, kTile * CT, (int)(blockIdx.x / (unsigned)pa.n_tiles), &expert,
-                              &first, &end))
-        return;
     const int nt = (int)(blockIdx.x % (unsigned)pa.n_tiles);
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
@@ -646,7 +642,19 @@ template <int Q, int CT, int KW, bool GEN>
 __global__ __launch_bounds__(kThreads, CT == 1 && Q <= 4 && !GEN ? 4 : 2)
 void k_panel(Args pa) {
     __shared__ uint4 xbuf[KW * 2 * CT * 512];
-    body<Q, CT, KW, GEN>(pa, xbuf);
+    int expert, first, end;
+    if (!sa_linear::find_tile(pa.a, kTile * CT, (int)(blockIdx.x / (unsigned)pa.n_tiles), &expert,
+                              &first, &end))
+        return;
+    // a tile of fewer rows runs the body of their height
+    const int rows = end - first;
+    if constexpr (CT == 8) {
+        if (rows <= 2 * kTile) return body<Q, 2, KW, GEN>(pa, xbuf, expert, first, end);
+        if (rows <= 4 * kTile) return body<Q, 4, KW, GEN>(pa, xbuf, expert, first, end);
+    } else if constexpr (CT == 4 || (CT == 2 && KW > 1)) {
+        if (rows <= CT / 2 * kTile) return body<Q, CT / 2, KW, GEN>(pa, xbuf, expert, first, end);
+    }
+    body<Q, CT, KW, GEN>(pa, xbuf, expert, first, end);
 }
 
 template <int Q, int CT, int KW, bool GEN>

@@ -1,6 +1,8 @@
 // A router's choice of experts and the sum of the experts' rows.
 #include <hip/hip_runtime.h>
 
+#include <type_traits>
+
 #include "checks.h"
 #include "epilogue.h"
 #include "keys.h"
@@ -15,12 +17,12 @@ namespace {
 // order; 0 stands for -inf, NaN and what was chosen before.
 //
 // The lists.  Tokens are dealt to at most kMaxBlocks workgroups in ranges of whole
-// 64-token steps.  Each workgroup counts its choices by expert (k_choose); a second
+// 32-token steps.  Each workgroup counts its choices by expert (k_choose); a second
 // launch (k_place) adds up the counts of the workgroups before it and of all experts
 // below, and gives every choice its place: a step's choices of an expert are one bit a
-// token in a 64-bit mask, the place is the number of bits below.  Nothing depends on
+// token in a 32-bit mask, the place is the number of bits below.  Nothing depends on
 // the order of atomics.  Up to kOneBlock tokens one workgroup does both.
-constexpr int kStep = 64;         // tokens of a step
+constexpr int kStep = 32;         // tokens of a step
 constexpr int kMaxBlocks = 256;
 constexpr int kWaves = 16;
 constexpr int kThreads = 64 * kWaves;
@@ -48,10 +50,19 @@ __device__ inline float logit_of(uint32_t o) {
     return __builtin_bit_cast(float, o & 0x80000000u ? o & 0x7fffffffu : ~o);
 }
 
+// The largest of the wave's values, the same in every lane: within 16 lanes, then across.
 __device__ inline uint32_t wave_max(uint32_t v) {
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) v = max(v, (uint32_t)__shfl_xor((int)v, d));
-    return v;
+    auto from = [&](auto control) {
+        return (uint32_t)__builtin_amdgcn_update_dpp((int)v, (int)v, decltype(control)::value, 0xf, 0xf,
+                                                     false);
+    };
+    v = max(v, from(std::integral_constant<int, 0xB1>{}));   // lanes 1, 0, 3, 2
+    v = max(v, from(std::integral_constant<int, 0x4E>{}));   // lanes 2, 3, 0, 1
+    v = max(v, from(std::integral_constant<int, 0x141>{}));  // halves of 8 mirrored
+    v = max(v, from(std::integral_constant<int, 0x140>{}));  // 16 mirrored
+    v = max(v, from(std::integral_constant<int, 0x142>{}));  // the 16 lanes before
+    v = max(v, from(std::integral_constant<int, 0x143>{}));  // the 32 lanes before
+    return (uint32_t)__builtin_amdgcn_readlane((int)v, 63);
 }
 
 __device__ inline float wave_sum(float v) {
@@ -101,7 +112,7 @@ __device__ inline int choose(const Route& a, int t) {
             rest = max(rest, o[p]);
         }
         best = rest;
-        e = __shfl(e, from);
+        e = __builtin_amdgcn_readlane(e, from);
         if (lane == j) {
             id = e;
             w = expf(logit_of(top) - peak);
@@ -117,32 +128,29 @@ __device__ inline int choose(const Route& a, int t) {
     return id;
 }
 
-// Places of the tokens [t0, t1): base[e] holds the first free slot of expert e, mask
-// two words an expert.
+// Places of the tokens [t0, t1): base[e] holds the first free slot of expert e.
 __device__ inline void place(const Route& a, int t0, int t1, int* base, uint32_t* mask) {
     for (int s = t0; s < t1; s += kStep) {
-        for (int i = threadIdx.x; i < 2 * a.experts; i += kThreads) mask[i] = 0u;
+        for (int e = threadIdx.x; e < a.experts; e += kThreads) mask[e] = 0u;
         __syncthreads();
         const int items = imin(kStep, t1 - s) * a.k;
         const int64_t i0 = (int64_t)s * a.k;
         for (int i = threadIdx.x; i < items; i += kThreads) {
-            const int e = a.ids[i0 + i], t = i / a.k;
-            if (e >= 0) atomicOr(&mask[2 * e + (t >> 5)], 1u << (t & 31));
+            const int e = a.ids[i0 + i];
+            if (e >= 0) atomicOr(&mask[e], 1u << (i / a.k));
         }
         __syncthreads();
         for (int i = threadIdx.x; i < items; i += kThreads) {
             const int e = a.ids[i0 + i], t = i / a.k;
             int slot = -1;
             if (e >= 0) {
-                const uint64_t m = (uint64_t)mask[2 * e + 1] << 32 | mask[2 * e];
-                slot = base[e] + __popcll(m & (((uint64_t)1 << t) - 1));
+                slot = base[e] + __popc(mask[e] & ((1u << t) - 1u));
                 a.row_of[slot] = s + t;
             }
             a.slot_of[i0 + i] = slot;
         }
         __syncthreads();
-        for (int e = threadIdx.x; e < a.experts; e += kThreads)
-            base[e] += __popc(mask[2 * e]) + __popc(mask[2 * e + 1]);
+        for (int e = threadIdx.x; e < a.experts; e += kThreads) base[e] += __popc(mask[e]);
         __syncthreads();
     }
 }
@@ -176,7 +184,7 @@ template <int PER, bool ALL>
 __global__ __launch_bounds__(kThreads) void k_choose(Route a) {
     __shared__ int counts[64 * PER];
     __shared__ int base[ALL ? 64 * PER : 1];
-    __shared__ uint32_t mask[ALL ? 2 * 64 * PER : 1];
+    __shared__ uint32_t mask[ALL ? 64 * PER : 1];
     const int wave = threadIdx.x >> 6;
     for (int e = threadIdx.x; e < a.experts; e += kThreads) {
         counts[e] = 0;
@@ -203,17 +211,23 @@ __global__ __launch_bounds__(kThreads) void k_choose(Route a) {
 __global__ __launch_bounds__(kThreads) void k_place(Route a) {
     __shared__ int total[SA_MAX_EXPERTS];
     __shared__ int base[SA_MAX_EXPERTS];
-    __shared__ uint32_t mask[2 * SA_MAX_EXPERTS];
+    __shared__ uint32_t mask[SA_MAX_EXPERTS];
     const int blocks = (int)gridDim.x;
-    for (int e = threadIdx.x; e < a.experts; e += kThreads) {
+    for (int e = threadIdx.x; e < a.experts; e += kThreads) base[e] = total[e] = 0;
+    __syncthreads();
+    // the threads of an expert share the workgroups' counts (integers: any order)
+    const int shares = imax(1, kThreads / a.experts);
+    for (int i = threadIdx.x; i < shares * a.experts; i += kThreads) {
+        const int e = i % a.experts;
         int below = 0, all = 0;
-        for (int b = 0; b < blocks; ++b) {
+#pragma unroll 4
+        for (int b = i / a.experts; b < blocks; b += shares) {
             const int v = a.counts[(int64_t)b * a.experts + e];
-            if (b < (int)blockIdx.x) below += v;
+            below += b < (int)blockIdx.x ? v : 0;
             all += v;
         }
-        base[e] = below;
-        total[e] = all;
+        atomicAdd(&base[e], below);
+        atomicAdd(&total[e], all);
     }
     __syncthreads();
     const int all = add_below(a.experts, total, base, blockIdx.x == 0 ? a.offsets : nullptr);
@@ -264,23 +278,69 @@ struct Combine {
     int slots, k, N, half;
 };
 
-// A workgroup takes kCols columns of one token, a thread every 256th of them.
+// A workgroup takes kCols columns of one token, a thread 8 consecutive ones: four rows are
+// requested at a time.  Bound by memory: every row of h is read once.
 constexpr int kCols = 2048;
+
+template <typename T>
+__device__ inline void combine(const Combine& a, int64_t t, int n) {
+    typedef T vec_t __attribute__((ext_vector_type(8), aligned(sizeof(T))));
+    const T* h = static_cast<const T*>(a.h);
+    const int64_t at = t * a.N + n;
+    const int count = imin(8, a.N - n);
+    auto load = [&](const T* p) {
+        vec_t v;
+        if (count == 8) {
+            v = *reinterpret_cast<const vec_t*>(p);
+        } else {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] = j < count ? p[j] : (T)0;
+        }
+        return v;
+    };
+    float sum[8] = {};
+    if (a.residual) {
+        const vec_t r = load(static_cast<const T*>(a.residual) + at);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) sum[j] = (float)r[j];
+    }
+    for (int j0 = 0; j0 < a.k; j0 += 4) {
+        vec_t row[4];
+        float w[4];
+        bool live[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            const int j = imin(j0 + u, a.k - 1);
+            const int slot = a.slot_of[t * a.k + j];
+            live[u] = j0 + u < a.k && slot >= 0 && slot < a.slots;
+            w[u] = a.weights[t * a.k + j];
+            if (live[u]) row[u] = load(h + (int64_t)slot * a.N + n);
+        }
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+            if (live[u])
+#pragma unroll
+                for (int j = 0; j < 8; ++j) sum[j] = fmaf(w[u], (float)row[u][j], sum[j]);
+    }
+    T* y = static_cast<T*>(a.y) + at;
+    if (count == 8) {
+        vec_t v;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = (T)sum[j];
+        *reinterpret_cast<vec_t*>(y) = v;
+    } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            if (j < count) y[j] = (T)sum[j];
+    }
+}
 
 __global__ __launch_bounds__(256) void k_combine(Combine a, int pieces) {
     const int64_t t = blockIdx.x / (unsigned)pieces;
-    const int n0 = (int)(blockIdx.x % (unsigned)pieces) * kCols;
-    const int n1 = imin(a.N - n0, kCols) + n0;
-    for (int n = n0 + (int)threadIdx.x; n < n1; n += 256) {
-        const int64_t i = t * a.N + n;
-        float v = a.residual ? sa_epi::load(a.residual, i, a.half) : 0.0f;
-        for (int j = 0; j < a.k; ++j) {
-            const int slot = a.slot_of[t * a.k + j];
-            if (slot < 0 || slot >= a.slots) continue;
-            v = fmaf(a.weights[t * a.k + j], sa_epi::load(a.h, (int64_t)slot * a.N + n, a.half), v);
-        }
-        sa_epi::store(a.y, i, v, a.half);
-    }
+    const int n = (int)(blockIdx.x % (unsigned)pieces) * kCols + 8 * (int)threadIdx.x;
+    if (n >= a.N) return;
+    if (a.half) combine<_Float16>(a, t, n);
+    else combine<float>(a, t, n);
 }
 
 bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
