@@ -11,9 +11,9 @@ namespace {
 
 // ---------------------------------------------------------------- choice
 //
-// A wave takes a token at a time, each lane PER consecutive experts.  The k largest
-// logits come one after the other: a maximum over the wave, the lowest lane that
-// holds it, its lowest expert.  Logits are compared as unsigned numbers of the same
+// A token belongs to 16 lanes (up to 256 experts) or to a wave, each lane PER
+// consecutive experts.  The k largest logits come one after the other: a maximum over
+// the lanes, then the lowest expert that holds it.  Logits are compared as unsigned numbers of the same
 // order; 0 stands for -inf, NaN and what was chosen before.
 //
 // The lists.  Tokens are dealt to at most kMaxBlocks workgroups in ranges of whole
@@ -24,8 +24,7 @@ namespace {
 // the order of atomics.  Up to kOneBlock tokens one workgroup does both.
 constexpr int kStep = 32;         // tokens of a step
 constexpr int kMaxBlocks = 256;
-constexpr int kWaves = 16;
-constexpr int kThreads = 64 * kWaves;
+constexpr int kThreads = 512;
 constexpr int kOneBlock = 64;     // tokens
 
 struct Route {
@@ -50,107 +49,115 @@ __device__ inline float logit_of(uint32_t o) {
     return __builtin_bit_cast(float, o & 0x80000000u ? o & 0x7fffffffu : ~o);
 }
 
-// The largest of the wave's values, the same in every lane: within 16 lanes, then across.
-__device__ inline uint32_t wave_max(uint32_t v) {
-    auto from = [&](auto control) {
-        return (uint32_t)__builtin_amdgcn_update_dpp((int)v, (int)v, decltype(control)::value, 0xf, 0xf,
-                                                     false);
+// op over the 16 lanes of a row, or over the wave, in every lane: quads, halves of 8 and 16
+// mirrored, then the rows in order.
+template <int LANES, typename T, typename F>
+__device__ inline T reduce(T v, F op) {
+    auto moved = [&](auto control) {
+        return __builtin_bit_cast(
+            T, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, v), decltype(control)::value, 0xf, 0xf,
+                                        true));
     };
-    v = max(v, from(std::integral_constant<int, 0xB1>{}));   // lanes 1, 0, 3, 2
-    v = max(v, from(std::integral_constant<int, 0x4E>{}));   // lanes 2, 3, 0, 1
-    v = max(v, from(std::integral_constant<int, 0x141>{}));  // halves of 8 mirrored
-    v = max(v, from(std::integral_constant<int, 0x140>{}));  // 16 mirrored
-    v = max(v, from(std::integral_constant<int, 0x142>{}));  // the 16 lanes before
-    v = max(v, from(std::integral_constant<int, 0x143>{}));  // the 32 lanes before
-    return (uint32_t)__builtin_amdgcn_readlane((int)v, 63);
-}
-
-__device__ inline float wave_sum(float v) {
+    v = op(v, moved(std::integral_constant<int, 0xB1>{}));
+    v = op(v, moved(std::integral_constant<int, 0x4E>{}));
+    v = op(v, moved(std::integral_constant<int, 0x141>{}));
+    v = op(v, moved(std::integral_constant<int, 0x140>{}));
+    if constexpr (LANES == 64) {
+        T r[4];
 #pragma unroll
-    for (int d = 1; d < 64; d <<= 1) v += __shfl_xor(v, d);
+        for (int i = 0; i < 4; ++i)
+            r[i] = __builtin_bit_cast(
+                T, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), 16 * i));
+        v = op(op(r[0], r[1]), op(r[2], r[3]));
+    }
     return v;
 }
 
-// Token t's choices: lane j < k returns the expert of choice j, or -1.
-template <int PER>
-__device__ inline int choose(const Route& a, int t) {
-    const int lane = threadIdx.x & 63;
+// Token t's choices by LANES lanes, this one `lane` of them: lane j < k returns the expert
+// of choice j, or -1.  All lanes call it; live = false: no token.
+template <int LANES, int PER>
+__device__ inline int choose(const Route& a, int t, int lane, bool live) {
+    const auto larger = [](uint32_t x, uint32_t y) { return max(x, y); };
+    const auto smaller = [](int x, int y) { return min(x, y); };
+    const auto plus = [](float x, float y) { return x + y; };
     const float* l = a.logits + (int64_t)t * a.experts;
     uint32_t o[PER];
 #pragma unroll
     for (int p = 0; p < PER; ++p) {
         const int e = PER * lane + p;
-        o[p] = e < a.experts ? order_of(l[e]) : 0u;
+        o[p] = live && e < a.experts ? order_of(l[e]) : 0u;
     }
     uint32_t best = 0;
 #pragma unroll
     for (int p = 0; p < PER; ++p) best = max(best, o[p]);
-    const uint32_t first = wave_max(best);
-    const float peak = first ? logit_of(first) : 0.0f;
+    uint32_t top = reduce<LANES>(best, larger);
+    const float peak = top ? logit_of(top) : 0.0f;
     float total = 0.0f;
     if (!a.normalize) {
 #pragma unroll
         for (int p = 0; p < PER; ++p)
             if (o[p]) total += expf(logit_of(o[p]) - peak);
-        total = wave_sum(total);
+        total = reduce<LANES>(total, plus);
     }
     int id = -1;
-    float w = 0.0f;
-    uint32_t top = first;
-    for (int j = 0; j < a.k && top; ++j) {
-        const int from = __builtin_ctzll(__ballot(best == top));
-        int e = 0;
-        bool open = lane == from;
-        uint32_t rest = 0;
+    uint32_t mine = 0;
+    for (int j = 0; j < a.k; ++j) {
+        // the lowest expert that holds it; none left: every expert is past the last
+        int e = a.experts;
+#pragma unroll
+        for (int p = PER - 1; p >= 0; --p)
+            if (top && o[p] == top) e = PER * lane + p;
+        e = reduce<LANES>(e, smaller);
+        if (lane == j && top) {
+            id = e;
+            mine = top;
+        }
+        best = 0;
 #pragma unroll
         for (int p = 0; p < PER; ++p) {
-            if (open && o[p] == top) {
-                e = PER * lane + p;
-                o[p] = 0;
-                open = false;
-            }
-            rest = max(rest, o[p]);
+            o[p] = PER * lane + p == e ? 0u : o[p];
+            best = max(best, o[p]);
         }
-        best = rest;
-        e = __builtin_amdgcn_readlane(e, from);
-        if (lane == j) {
-            id = e;
-            w = expf(logit_of(top) - peak);
-        }
-        top = wave_max(best);
+        top = reduce<LANES>(best, larger);
     }
-    if (a.normalize) total = wave_sum(w);
-    if (lane < a.k) {
+    const float w = mine ? expf(logit_of(mine) - peak) : 0.0f;
+    if (a.normalize) total = reduce<LANES>(w, plus);
+    if (live && lane < a.k) {
         const int64_t i = (int64_t)t * a.k + lane;
         a.ids[i] = id;
         a.weights[i] = id < 0 ? 0.0f : w / total;
     }
-    return id;
+    return live ? id : -1;
 }
 
-// Places of the tokens [t0, t1): base[e] holds the first free slot of expert e.
-__device__ inline void place(const Route& a, int t0, int t1, int* base, uint32_t* mask) {
+// The expert of this thread's choice in the step of tokens [s, t1), or -1.
+static_assert(kStep * SA_MAX_CHOICES <= kThreads, "one choice a thread and step");
+__device__ inline int choice_of(const Route& a, int s, int t1) {
+    const int items = imin(kStep, t1 - s) * a.k;
+    return (int)threadIdx.x < items ? a.ids[(int64_t)s * a.k + threadIdx.x] : -1;
+}
+
+// Places of the tokens [t0, t1): base[e] holds the first free slot of expert e, `e` this
+// thread's choice of the first step.
+__device__ inline void place(const Route& a, int t0, int t1, int e, int* base, uint32_t* mask) {
+    const int t = (int)threadIdx.x / a.k;
     for (int s = t0; s < t1; s += kStep) {
-        for (int e = threadIdx.x; e < a.experts; e += kThreads) mask[e] = 0u;
+        for (int i = threadIdx.x; i < a.experts; i += kThreads) mask[i] = 0u;
         __syncthreads();
-        const int items = imin(kStep, t1 - s) * a.k;
-        const int64_t i0 = (int64_t)s * a.k;
-        for (int i = threadIdx.x; i < items; i += kThreads) {
-            const int e = a.ids[i0 + i];
-            if (e >= 0) atomicOr(&mask[e], 1u << (i / a.k));
-        }
+        if (e >= 0) atomicOr(&mask[e], 1u << t);
         __syncthreads();
-        for (int i = threadIdx.x; i < items; i += kThreads) {
-            const int e = a.ids[i0 + i], t = i / a.k;
+        if ((int)threadIdx.x < imin(kStep, t1 - s) * a.k) {
             int slot = -1;
             if (e >= 0) {
                 slot = base[e] + __popc(mask[e] & ((1u << t) - 1u));
                 a.row_of[slot] = s + t;
             }
-            a.slot_of[i0 + i] = slot;
+            a.slot_of[(int64_t)s * a.k + threadIdx.x] = slot;
         }
+        if (s + kStep >= t1) break;
+        e = choice_of(a, s + kStep, t1);
         __syncthreads();
-        for (int e = threadIdx.x; e < a.experts; e += kThreads) base[e] += __popc(mask[e]);
+        for (int i = threadIdx.x; i < a.experts; i += kThreads) base[i] += __popc(mask[i]);
         __syncthreads();
     }
 }
@@ -180,27 +187,27 @@ __device__ inline int add_below(int experts, const int* total, int* base, int* o
     return before;
 }
 
-template <int PER, bool ALL>
+template <int LANES, int PER, bool ALL>
 __global__ __launch_bounds__(kThreads) void k_choose(Route a) {
-    __shared__ int counts[64 * PER];
-    __shared__ int base[ALL ? 64 * PER : 1];
-    __shared__ uint32_t mask[ALL ? 64 * PER : 1];
-    const int wave = threadIdx.x >> 6;
+    __shared__ int counts[LANES * PER];
+    __shared__ int base[ALL ? LANES * PER : 1];
+    __shared__ uint32_t mask[ALL ? LANES * PER : 1];
     for (int e = threadIdx.x; e < a.experts; e += kThreads) {
         counts[e] = 0;
         if constexpr (ALL) base[e] = 0;
     }
     __syncthreads();
     const int t0 = (int)blockIdx.x * a.per_block, t1 = imin(t0 + a.per_block, a.tokens);
-    for (int t = t0 + wave; t < t1; t += kWaves) {
-        const int id = choose<PER>(a, t);
+    for (int s = t0; s < t1; s += kThreads / LANES) {
+        const int t = s + (int)threadIdx.x / LANES;
+        const int id = choose<LANES, PER>(a, imin(t, t1 - 1), (int)threadIdx.x % LANES, t < t1);
         if (id >= 0) atomicAdd(&counts[id], 1);
     }
     __syncthreads();
     if constexpr (ALL) {
         const int all = add_below(a.experts, counts, base, a.offsets);
         __syncthreads();
-        place(a, 0, a.tokens, base, mask);
+        place(a, 0, a.tokens, choice_of(a, 0, a.tokens), base, mask);
         for (int i = all + threadIdx.x; i < a.tokens * a.k; i += kThreads) a.row_of[i] = -1;
     } else {
         for (int e = threadIdx.x; e < a.experts; e += kThreads)
@@ -213,6 +220,8 @@ __global__ __launch_bounds__(kThreads) void k_place(Route a) {
     __shared__ int base[SA_MAX_EXPERTS];
     __shared__ uint32_t mask[SA_MAX_EXPERTS];
     const int blocks = (int)gridDim.x;
+    const int t0 = (int)blockIdx.x * a.per_block, t1 = imin(t0 + a.per_block, a.tokens);
+    const int first = choice_of(a, t0, t1);
     for (int e = threadIdx.x; e < a.experts; e += kThreads) base[e] = total[e] = 0;
     __syncthreads();
     // the threads of an expert share the workgroups' counts (integers: any order)
@@ -220,7 +229,7 @@ __global__ __launch_bounds__(kThreads) void k_place(Route a) {
     for (int i = threadIdx.x; i < shares * a.experts; i += kThreads) {
         const int e = i % a.experts;
         int below = 0, all = 0;
-#pragma unroll 4
+#pragma unroll 16
         for (int b = i / a.experts; b < blocks; b += shares) {
             const int v = a.counts[(int64_t)b * a.experts + e];
             below += b < (int)blockIdx.x ? v : 0;
@@ -232,8 +241,7 @@ __global__ __launch_bounds__(kThreads) void k_place(Route a) {
     __syncthreads();
     const int all = add_below(a.experts, total, base, blockIdx.x == 0 ? a.offsets : nullptr);
     __syncthreads();
-    const int t0 = (int)blockIdx.x * a.per_block, t1 = imin(t0 + a.per_block, a.tokens);
-    place(a, t0, t1, base, mask);
+    place(a, t0, t1, first, base, mask);
     const int64_t n = (int64_t)a.tokens * a.k;
     for (int64_t i = all + (int64_t)blockIdx.x * kThreads + threadIdx.x; i < n;
          i += (int64_t)blocks * kThreads)
@@ -257,13 +265,13 @@ bool route_sizes(int tokens, int experts, int k) {
            k >= 1 && k <= experts && k <= SA_MAX_CHOICES;
 }
 
-template <int PER>
+template <int LANES, int PER>
 void launch_route(const Route& a, int blocks, hipStream_t s) {
     if (blocks == 1) {
-        hipLaunchKernelGGL((k_choose<PER, true>), dim3(1), dim3(kThreads), 0, s, a);
+        hipLaunchKernelGGL((k_choose<LANES, PER, true>), dim3(1), dim3(kThreads), 0, s, a);
         return;
     }
-    hipLaunchKernelGGL((k_choose<PER, false>), dim3(blocks), dim3(kThreads), 0, s, a);
+    hipLaunchKernelGGL((k_choose<LANES, PER, false>), dim3(blocks), dim3(kThreads), 0, s, a);
     hipLaunchKernelGGL(k_place, dim3(blocks), dim3(kThreads), 0, s, a);
 }
 
@@ -373,12 +381,12 @@ SA_API int sa_route_experts(const float* logits, int tokens, int experts, int k,
                static_cast<int32_t*>(workspace), 0};
     const int blocks = route_blocks(tokens, &a.per_block);
     hipStream_t s = reinterpret_cast<hipStream_t>(stream);
-    const int per = (experts + 63) / 64;
-    if (per == 1) launch_route<1>(a, blocks, s);
-    else if (per == 2) launch_route<2>(a, blocks, s);
-    else if (per <= 4) launch_route<4>(a, blocks, s);
-    else if (per <= 8) launch_route<8>(a, blocks, s);
-    else launch_route<16>(a, blocks, s);
+    if (experts <= 16) launch_route<16, 1>(a, blocks, s);
+    else if (experts <= 64) launch_route<16, 4>(a, blocks, s);
+    else if (experts <= 128) launch_route<16, 8>(a, blocks, s);
+    else if (experts <= 256) launch_route<16, 16>(a, blocks, s);
+    else if (experts <= 512) launch_route<64, 8>(a, blocks, s);
+    else launch_route<64, 16>(a, blocks, s);
     return launch_status();
 }
 
