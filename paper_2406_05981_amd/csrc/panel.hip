@@ -335,6 +335,23 @@ __device__ __forceinline__ void body(const Args& pa, uint4* xbuf, int expert, in
         W[0] = cat(x.p[0]);
         W[1] = cat(x.p[1]);
     };
+    // (a block without the interleaving)
+    auto in_turn = [&](const uint4* xs, auto w, auto e) {
+        half8_t X[kRing], W[2];
+        Next x;
+        int xw;
+        first_x(xs, &xw, X);
+        new_block(x, e);
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+#pragma unroll
+            for (int u = 0; u < kPieces; ++u) piece(x, u, q, w);
+            take(x, W);
+            __builtin_amdgcn_sched_barrier(0);
+            products(xs, xw, q, W, X);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    };
     auto quarter = [&](const uint4* xs, int xw, int q, const half8_t (&W)[2], half8_t (&X)[kRing],
                        auto next) {
         constexpr int n = 2 * CT;
@@ -410,6 +427,10 @@ __device__ __forceinline__ void body(const Args& pa, uint4* xbuf, int expert, in
         }
     };
 
+    // a row's 16 keys of a block are stored rotated by the row
+    const uint32_t rot = (uint32_t)(16 - (n & 15)) & 15u;
+    const uint32_t rot_bytes = rot & 3u, rot_bits = 4u * (rot & 4u);
+    const bool rot_swap = rot & 8u;
     // A group of two blocks as words in step order: wd[block][plane][half], ew the planes'
     // exponents of a block; returns whether this lane's row has a block to do plane by plane.
     auto unpack = [&](const Keys<Q, GEN>& k, uint32_t (&wd)[2][Q][2], uint32_t (&ew)[2][kE]) {
@@ -417,14 +438,30 @@ __device__ __forceinline__ void body(const Args& pa, uint4* xbuf, int expert, in
         uint32_t own[kE] = {};
 #pragma unroll
         for (int i = 0; i < Q; ++i) {
-            uint32_t c[4];
-            rotate16(k.w[i], 16 - (n & 15), c);
-            // even and odd chunks; lanes 0-31 keep the even ones of both blocks
+            // rotated by rot: the part of whole bytes first, then even and odd chunks as two
+            // rows of 8 bytes, each by half of the rest
+            const uint32_t in[4] = {k.w[i].x, k.w[i].y, k.w[i].z, k.w[i].w};
+            uint32_t c[4], ev[2], od[2];
+#pragma unroll
+            for (int d = 0; d < 4; ++d)
+                c[d] = __builtin_amdgcn_alignbyte(in[(d + 1) & 3], in[d], rot_bytes);
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                const uint32_t ev = __builtin_amdgcn_perm(c[2 * h + 1], c[2 * h], 0x06040200u);
-                const uint32_t od = __builtin_amdgcn_perm(c[2 * h + 1], c[2 * h], 0x07050301u);
-                const auto sw = __builtin_amdgcn_permlane32_swap(ev, od, false, false);
+                ev[h] = __builtin_amdgcn_perm(c[2 * h + 1], c[2 * h], 0x06040200u);
+                od[h] = __builtin_amdgcn_perm(c[2 * h + 1], c[2 * h], 0x07050301u);
+            }
+            auto turn = [&](uint32_t (&v)[2]) {
+                const uint32_t lo = __builtin_amdgcn_alignbit(v[1], v[0], rot_bits);
+                const uint32_t hi = __builtin_amdgcn_alignbit(v[0], v[1], rot_bits);
+                v[0] = rot_swap ? hi : lo;
+                v[1] = rot_swap ? lo : hi;
+            };
+            turn(ev);
+            turn(od);
+            // lanes 0-31 keep the even chunks of both blocks, lanes 32-63 the odd ones
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const auto sw = __builtin_amdgcn_permlane32_swap(ev[h], od[h], false, false);
                 wd[0][i][h] = sw[0];
                 wd[1][i][h] = sw[1];
             }
@@ -513,7 +550,8 @@ __device__ __forceinline__ void body(const Args& pa, uint4* xbuf, int expert, in
                     }
                 }
             } else if (run) {
-                summed(J0, xr, w0, e0);
+                if constexpr (Q <= 4) in_turn(xr, w0, e0);
+                else summed(J0, xr, w0, e0);
             }
             arrive();
             if (s0 + 1 >= steps) break;
@@ -532,6 +570,8 @@ __device__ __forceinline__ void body(const Args& pa, uint4* xbuf, int expert, in
                             if (q < 3) piece(x, u, q + 1, w1);
                         });
                     }
+                } else if constexpr (Q <= 4) {
+                    in_turn(xs, w1, e1);
                 } else {
                     summed(J0 + 1, xs, w1, e1);
                 }
