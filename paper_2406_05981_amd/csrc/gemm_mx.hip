@@ -546,10 +546,10 @@ __device__ __forceinline__ void body(const KernelArgs& ka, char* lds, int wg,
     }
 }
 
-template <int CT>
+template <int CT, int WAVES = kWaves>
 constexpr int lds_bytes() {
-    const int pieces = kWaves * (kPieces * 4 * CT * kColBytes + 4 * CT * 16);
-    const int red = kWaves * kMaxTiles * CT * 256;
+    const int pieces = WAVES * (kPieces * 4 * CT * kColBytes + 4 * CT * 16);
+    const int red = WAVES * kMaxTiles * CT * 256;
     return pieces > red ? pieces : red;
 }
 
@@ -566,13 +566,17 @@ __global__ __launch_bounds__(kThreads, 2) void k_gemm_mx_epilogue(KernelArgs a, 
     body<Q, CT, NP, false, true>(a, reinterpret_cast<char*>(lds), (int)blockIdx.x, rows);
 }
 
-// Experts of at most kExpertRows rows (the others are left to the panel kernel):
-// workgroups wgs * e ... have expert e, in the form for its number of rows.
+// Experts of at most kExpertRows rows (the others are left to the panel kernel), four rows
+// at a time: workgroups wgs * e ... have expert e.  An expert's few tiles are a chain of
+// latencies, so three workgroups of four waves a CU (170 registers) gain more than one of
+// eight waves or eight rows at a time; a second pass over the same tiles finds their keys
+// in the cache.
+constexpr int kExpertWaves = 4;
 template <int Q>
-__global__ __launch_bounds__(kThreads, 2) void k_gemm_mx_experts(KernelArgs ka, Rows rows,
+__global__ __launch_bounds__(64 * kExpertWaves, 3) void k_gemm_mx_experts(KernelArgs ka, Rows rows,
                                                                  const int32_t* offsets, int slots,
                                                                  int wgs) {
-    __shared__ uint4 lds[(lds_bytes<2>() + 15) / 16];
+    __shared__ uint4 lds[(lds_bytes<1, kExpertWaves>() + 15) / 16];
     const int e = (int)(blockIdx.x / (unsigned)wgs), wg = (int)(blockIdx.x % (unsigned)wgs);
     const int lo = imin(imax(offsets[e], 0), slots);
     const int count = imin(imax(offsets[e + 1], lo), slots) - lo;
@@ -581,13 +585,14 @@ __global__ __launch_bounds__(kThreads, 2) void k_gemm_mx_experts(KernelArgs ka, 
     const int64_t nk = (int64_t)a.q * a.N;
     a.packed += e * nk * (a.K >> 3);
     a.exps += e * nk * ka.NG;
-    a.B = count;
-    rows.first = lo;
     if (rows.epi.bias) rows.epi.bias += (int64_t)e * a.N;
-    char* l = reinterpret_cast<char*>(lds);
-    if (count <= 2) body<Q, 1, 1, false, true>(ka, l, wg, rows);
-    else if (count <= 4) body<Q, 1, 2, false, true>(ka, l, wg, rows);
-    else body<Q, 2, 4, false, true>(ka, l, wg, rows);
+#pragma unroll 1
+    for (int b = 0; b < count; b += 4) {
+        if (b) __syncthreads();
+        a.B = imin(4, count - b);
+        rows.first = lo + b;
+        body<Q, 1, 2, false, true>(ka, reinterpret_cast<char*>(lds), wg, rows);
+    }
 }
 
 // ---------------------------------------------------------------- choice and launch
@@ -701,11 +706,19 @@ void launch(const sa_linear::Layer& l, const sa_matrix_plan& p, hipStream_t s) {
     else launch_epilogue<2, 4>(ka, rows, p.workgroups, s);
 }
 
-// Every expert gets the workgroups of a layer of 8 rows.
+// Workgroups of 2 to kMaxTiles row tiles, enough of them for a few active experts.
 bool launch_experts(const sa_linear::Layer& l, hipStream_t s) {
     sa_matrix_plan p;
     if (l.q > 4 || l.G % 128 || plan(l.q, l.N, l.K, l.G, kExpertRows, 0, &p) >= sa_matrix::kNever)
         return false;
+    const int groups = (l.K / 128 + kGroupBlocks - 1) / kGroupBlocks;
+    p.column_shares = 1;
+    while (p.column_shares < kExpertWaves && p.column_shares < groups) p.column_shares *= 2;
+    const int sets = kExpertWaves / p.column_shares, tiles = (l.N + kTile - 1) / kTile;
+    p.threads = 64 * kExpertWaves;
+    const int active = imin(l.experts, l.rows);
+    int per = sets * imin(imax((int)((int64_t)tiles * active / (sets * 1536)), 2), kMaxTiles);
+    p.workgroups = (tiles + per - 1) / per;
     const KernelArgs ka = kernel_args(matrix_args(l), p);
     const Rows rows = {l.epi, l.row_of, 0, l.x_rows};
     const dim3 g((unsigned)p.workgroups * (unsigned)l.experts), b(p.threads);
