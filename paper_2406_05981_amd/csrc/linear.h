@@ -25,9 +25,10 @@ struct Layer {
     sa_epi::Epilogue epi;
 };
 
-// The `tile`-th tile of `height` rows, counted over the experts' rows, whole tiles of all
-// experts before the shorter ones at their ends: its expert and rows [first, end).  Every
-// lane of a wave calls it; false past the last tile.
+// The `tile`-th tile of `height` rows, counted over the experts' rows: whole tiles of all
+// experts first, then those at their ends of more than half the height, then the others (the
+// shortest run last).  Its expert and rows [first, end).  Every lane of a wave calls it;
+// false past the last tile.
 __device__ inline bool find_tile(const Layer& a, int height, int tile, int* expert, int* first,
                                  int* end) {
     if (!a.offsets) {
@@ -38,7 +39,7 @@ __device__ inline bool find_tile(const Layer& a, int height, int tile, int* expe
     }
     const int lane = threadIdx.x & 63;
     int before = 0;  // tiles counted
-    for (int whole = 1; whole >= 0; --whole)
+    for (int kind = 0; kind < 3; ++kind)
         for (int e0 = 0; e0 < a.experts; e0 += 64) {
             const int e = e0 + lane;
             int lo = 0, hi = 0;
@@ -47,8 +48,11 @@ __device__ inline bool find_tile(const Layer& a, int height, int tile, int* expe
                 hi = imin(imax(a.offsets[e + 1], lo), a.rows);
             }
             const int rows = hi - lo > a.few ? hi - lo : 0;
-            const int tiles = whole ? rows / height : (int)(rows % height != 0);
-            if (!whole) lo += rows / height * height;
+            const int rest = rows % height;
+            const int tiles = kind == 0   ? rows / height
+                              : kind == 1 ? (int)(2 * rest > height)
+                                          : (int)(rest > 0 && 2 * rest <= height);
+            if (kind) lo += rows - rest;
             int sum = tiles;
 #pragma unroll
             for (int d = 1; d < 64; d <<= 1) {
