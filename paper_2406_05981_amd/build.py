@@ -16,12 +16,13 @@ import sys
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 SOURCES = [os.path.join(HERE, "csrc", name)
-           for name in ("shiftadd.hip", "gemm_mx.hip", "gemm_mfma.hip", "linear.hip", "panel.hip", "route.hip",
+           for name in ("shiftadd.hip", "gemm_mx.hip", "gemm_mfma.hip", "linear.hip", "panel.hip",
+                        "panel_groups.hip", "route.hip",
                         "bcq.hip", "alloc.hip")]
 INCLUDE = os.path.join(ROOT, "include")
 HEADERS = [os.path.join(INCLUDE, "shiftadd.h")] + [
     os.path.join(HERE, "csrc", name)
-    for name in ("gemm_matrix.h", "keys.h", "checks.h", "epilogue.h", "linear.h")]
+    for name in ("gemm_matrix.h", "keys.h", "checks.h", "epilogue.h", "linear.h", "panel.h")]
 LIB = os.path.join(HERE, "libshiftadd.so")
 ARCH = "gfx950"
 

@@ -124,7 +124,8 @@ ACTS = ("none", "relu", "gelu", "gelu_tanh", "silu")
 LAYERS = [(3, 64, 128, 128), (3, 130, 256, 128), (2, 1509, 128, 128), (1, 16, 512, 256),
           (4, 100, 640, 128), (3, 257, 1152, 384), (5, 70, 384, 128), (8, 33, 256, 128),
           (3, 130, 256, 8), (2, 65, 136, 8), (3, 77, 264, 88), (3, 50, 192, 64), (1, 1, 8, 8),
-          (6, 48, 1040, 208), (2, 300, 4096, 128)]
+          (6, 48, 1040, 208), (2, 300, 4096, 128), (4, 45, 160, 32), (7, 40, 304, 16),
+          (2, 300, 960, 64), (1, 3, 64, 64), (3, 66, 2048, 64)]
 ROWS = [1, 2, 3, 8, 9, 16, 17, 33, 64, 65, 129, 250, 257, 300, 513]
 
 
@@ -150,7 +151,7 @@ def test_epilogue_terms(rows, act):
 def test_epilogue_exponent_ranges(rows, lo, hi):
     """Exponents far apart within a group and outside binary16's range."""
     for q, N, K, G in [(3, 70, 512, 128), (4, 40, 256, 256), (2, 33, 384, 128), (5, 40, 256, 128),
-                       (3, 40, 160, 32), (1, 64, 128, 128)]:
+                       (3, 40, 160, 32), (1, 64, 128, 128), (2, 40, 256, 8), (3, 40, 264, 88)]:
         run_epilogue(q, N, K, G, rows, "none", 0, 0, 0, 0, lo, hi)
 
 
@@ -300,7 +301,8 @@ COUNTS = [[1], [0], [0, 0, 3], [5, 0, 1, 2], [8, 1, 0, 0, 9, 16], [17, 0, 64, 1]
 @pytest.mark.parametrize("counts", COUNTS, ids=lambda c: "-".join(map(str, c[:6])) + f"-of{len(c)}")
 @pytest.mark.parametrize("gather", [0, 1])
 def test_experts(counts, gather):
-    layers = [(3, 64, 256, 128), (2, 133, 384, 128), (3, 65, 136, 8), (5, 48, 128, 128)]
+    layers = [(3, 64, 256, 128), (2, 133, 384, 128), (3, 65, 136, 8), (5, 48, 128, 128),
+              (1, 33, 192, 64)]
     for i, (q, N, K, G) in enumerate(layers):
         run_experts(q, N, K, G, counts, tokens=max(sum(counts), 7), gather=gather,
                     act=ACTS[(i + len(counts)) % 5], bias=i % 2, mul=(i + gather) % 2,
