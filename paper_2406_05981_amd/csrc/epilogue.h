@@ -27,6 +27,27 @@ __device__ inline float sigmoid(float z) {
     return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-1.44269504088896341f * z));
 }
 
+// v Phi(v) = v / 2 erfc(-v / sqrt 2).  erfc(z) = exp(-z^2) t P(t), t = 1 / (1 + z / 2), z >= 0, P
+// the polynomial of degree 8 closest to erfcx(z) / t (a least-squares fit, reweighted
+// towards equal relative errors: 3.2e-8; 3.0e-7 as evaluated in fp32); for v > 0 from the
+// other tail, 2 - erfc.  The library's erfcf has branches for every range: 45 million
+// outputs after a prompt's product cost 48 us with it.
+__device__ inline float gelu(float v) {
+    const float z = 0.70710678118654752f * fabsf(v);
+    const float t = __builtin_amdgcn_rcpf(fmaf(0.5f, z, 1.0f));
+    float p = -0.0555105545f;
+    p = fmaf(p, t, 0.266813397f);
+    p = fmaf(p, t, -0.449434638f);
+    p = fmaf(p, t, 0.233498693f);
+    p = fmaf(p, t, 0.00522376923f);
+    p = fmaf(p, t, 0.188610703f);
+    p = fmaf(p, t, 0.246851534f);
+    p = fmaf(p, t, 0.281826973f);
+    p = fmaf(p, t, 0.282120109f);
+    const float tail = p * t * __builtin_amdgcn_exp2f(-1.44269504088896341f * z * z);
+    return 0.5f * v * (v > 0.0f ? 2.0f - tail : tail);
+}
+
 template <int V>
 __device__ inline void activate(float (&v)[V], int act) {
     switch (act) {
@@ -35,9 +56,8 @@ __device__ inline void activate(float (&v)[V], int act) {
             for (int j = 0; j < V; ++j) v[j] = v[j] < 0.0f ? 0.0f : v[j];  // a NaN stays one
             break;
         case SA_ACT_GELU:
-            // the upper tail, not 1 + erf: no cancellation for negative v
 #pragma unroll
-            for (int j = 0; j < V; ++j) v[j] = 0.5f * v[j] * erfcf(-0.70710678118654752f * v[j]);
+            for (int j = 0; j < V; ++j) v[j] = gelu(v[j]);
             break;
         case SA_ACT_GELU_TANH:
             // 0.5 (1 + tanh u) = sigmoid(2 u)

@@ -291,11 +291,11 @@ struct Combine {
 constexpr int kCols = 2048;
 
 template <typename T>
-__device__ inline void combine(const Combine& a, int64_t t, int n) {
+__device__ inline void combine(const Combine& a, int64_t t, int64_t n) {
     typedef T vec_t __attribute__((ext_vector_type(8), aligned(sizeof(T))));
     const T* h = static_cast<const T*>(a.h);
     const int64_t at = t * a.N + n;
-    const int count = imin(8, a.N - n);
+    const int count = a.N - n < 8 ? (int)(a.N - n) : 8;
     auto load = [&](const T* p) {
         vec_t v;
         if (count == 8) {
@@ -345,7 +345,7 @@ __device__ inline void combine(const Combine& a, int64_t t, int n) {
 
 __global__ __launch_bounds__(256) void k_combine(Combine a, int pieces) {
     const int64_t t = blockIdx.x / (unsigned)pieces;
-    const int n = (int)(blockIdx.x % (unsigned)pieces) * kCols + 8 * (int)threadIdx.x;
+    const int64_t n = (int64_t)(blockIdx.x % (unsigned)pieces) * kCols + 8 * threadIdx.x;
     if (n >= a.N) return;
     if (a.half) combine<_Float16>(a, t, n);
     else combine<float>(a, t, n);
