@@ -10,6 +10,19 @@
 // 7e-6 of sum|terms| at 2^-24.)  A block of 128 columns
 // that has any other exponents in a wave's rows is left for a second loop, two products a
 // plane: +-2^e is a bfloat16 number, an activation the sum of two.
+//
+// Against a product a plane this takes a third of the matrix core's work for 3 planes and,
+// with tiles of 256 rows x 256 outputs, an expanded key serves 256 rows: layer of
+// 11008x4096, 3 planes, with SiLU and multiplier 4096 rows 401 us (922 TFLOP/s; a library
+// product of binary16 tensors of that size 425), 11003x4096 250 rows with GELU 46 us (the
+// tile kernel of gemm_mfma.hip 81 without).
+//
+// What bounds it.  4096 rows: power.  The same 258 thousand cycles of a 256-row tile take
+// 114 us on 64 compute units (2.26 GHz) and 140 us on all (1.84 GHz); the matrix cores are
+// busy 45% of the cycles, vector instructions 42%, 6.3 a product, of which 4.1 expand planes.
+// Up to 32 rows: vector instructions (4096x11008, 2 planes, 16 experts of 8 to 113 rows: 75%
+// of the SIMD cycles, matrix cores 19%).  Between: too few tiles for the compute units, 8
+// waves each, whose expansion, LDS reads and products follow each other at the barriers.
 #ifndef SHIFTADD_PANEL_H
 #define SHIFTADD_PANEL_H
 
@@ -119,6 +132,9 @@ struct Keys {
     uint32_t e[GEN == kWhole ? Q : 1];
 };
 
+// Why these tiles: keys are expanded once per tile of rows, so a wave's 128 accumulators go
+// into rows (256) before outputs (32); two waves a SIMD is what these registers leave.
+//
 // Work split.  Eight waves are RW sets of 32 outputs times KW shares of the columns; a
 // wave has all 32 CT rows of the workgroup.  Activations of a 128-column block lie in
 // LDS, double buffered and copied there without passing registers; the planes are
@@ -345,7 +361,8 @@ __device__ __forceinline__ void body(const Args& pa, uint4* xbuf, int expert, in
     };
     // The same with the next quarter's operands expanded between one quarter's products, a
     // piece after each: a product takes the matrix core 32 cycles, in which the two waves of
-    // a SIMD issue the expansion's vector instructions.  Pieces 0 .. Q - 1 spread a plane's
+    // a SIMD issue the expansion's vector instructions (11008x4096 4096 rows 386 -> 369 us;
+    // the compiler's own order of the same code puts the LDS reads last and gains nothing).  Pieces 0 .. Q - 1 spread a plane's
     // word, the others are a pair each, by the position of its bits (add_pair).
     struct Next {
         Spread sp[Q];

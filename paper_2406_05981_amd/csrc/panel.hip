@@ -81,6 +81,8 @@ void launch(const Layer& a, hipStream_t s) {
         case 2: start_form<2, kWhole>(pa, *f, s); break;
         case 3: start_form<3, kWhole>(pa, *f, s); break;
         case 4: start_form<4, kWhole>(pa, *f, s); break;
+        case 5:
+        case 6: start_form<6, kWhole>(pa, *f, s); break;
         default: start_form<8, kWhole>(pa, *f, s); break;
     }
 }

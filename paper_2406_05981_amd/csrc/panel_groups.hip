@@ -1,5 +1,8 @@
 // The layer for many rows (panel.h) where the groups are not whole blocks of 128 columns or
-// the columns end inside a block.
+// the columns end inside a block.  Groups of 8 to 64 columns load a row's 16 keys and the 16
+// exponents from a block's first on at once (4096x4096, 3 planes, group 64: 16 rows 57 -> 22
+// us, 1024 rows 222 -> 79 against a byte a chunk; k_gemm_generic 268 at 1 to 4 rows); what
+// is left over group 128 (8.7 and 50 us) is a factor a chunk and step.
 #include "panel.h"
 
 namespace sa_panel {
