@@ -251,6 +251,84 @@ def test_outputs_past_32_bit_offsets():
     check(y[pick], want, bound, "far rows")
 
 
+def test_most_rows():
+    q, N, K, G, rows = 2, 40, 64, 64, sa.SA_MAX_ROWS
+    packed, exps, W, F = make_layer(q, N, K, G)
+    x = torch.randn((rows, K), device="cuda", generator=gen(2)).half()
+    y = sa.shiftadd_linear(x, packed, exps, q, N, K, G, activation="relu")
+    check(y, *expected(x, W[0], F[0], q, None, "relu", None, None, 1), "2^20 rows")
+
+
+def test_long_rows():
+    """2^22 + 128 columns: past the bound of the kernels that divide by multiplication."""
+    q, N, K, G = 1, 17, (1 << 22) + 128, 128
+    packed, exps, W, F = make_layer(q, N, K, G)
+    for rows in (1, 3, 40):
+        x = torch.randn((rows, K), device="cuda", generator=gen(rows)).half()
+        y = sa.shiftadd_linear(x, packed, exps, q, N, K, G, out_dtype=torch.float32)
+        check(y, *expected(x, W[0], F[0], q, None, "none", None, None, 0), f"{rows} long rows")
+
+
+def test_activations_past_32_bit_offsets():
+    """Rows of x beyond 4 GiB, by a list and in order."""
+    q, N, K, G, rows = 2, 33, 8192, 128, 262144 + 300
+    packed, exps, W, F = make_layer(q, N, K, G)
+    x = torch.zeros((rows, K), dtype=torch.float16, device="cuda")
+    x[-300:] = torch.randn((300, K), device="cuda", generator=gen(4)).half()
+    slots = 300
+    row_of = torch.arange(rows - 1, rows - 1 - slots, -1, dtype=torch.int32, device="cuda")
+    offsets = torch.tensor([0, slots], dtype=torch.int32, device="cuda")
+    y = torch.empty((slots, N), device="cuda")
+    sa.sa_shiftadd_gemm_experts(x, row_of, offsets, packed, exps, q, N, K, G, 1, slots, None, "none",
+                                None, y)
+    want, bound = expected(x[row_of.long()], W[0], F[0], q, None, "none", None, None, 0)
+    check(y, want, bound, "far rows by a list")
+    full = sa.shiftadd_linear(x, packed, exps, q, N, K, G, out_dtype=torch.float32)
+    check(full[-slots:].flip(0), want, bound, "far rows in order")
+    assert (full[:-slots] == 0).all()
+
+
+@pytest.mark.parametrize("rows", [1, 6, 20, 90, 300])
+def test_epilogue_captured_and_replayed(rows):
+    q, N, K, G = 3, 200, 640, 128
+    packed, exps, _, _ = make_layer(q, N, K, G)
+    x = torch.zeros((rows, K), dtype=torch.float16, device="cuda")
+    res = torch.zeros((rows, N), dtype=torch.float16, device="cuda")
+    y = torch.empty_like(res)
+    call = lambda out: sa.sa_shiftadd_gemm_epilogue(  # noqa: E731
+        x, packed, exps, q, N, K, G, rows, None, "gelu", None, res, out)
+    call(y)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call(y)
+    for seed in range(3):
+        x.copy_(torch.randn((rows, K), device="cuda", generator=gen(seed)))
+        res.copy_(torch.randn((rows, N), device="cuda", generator=gen(seed + 9)))
+        graph.replay()
+        eager = torch.empty_like(y)
+        call(eager)
+        torch.cuda.synchronize()
+        assert torch.equal(y, eager)
+
+
+def test_calls_on_two_streams():
+    """Different calls in flight at once share nothing."""
+    q, N, K, G = 3, 1024, 1024, 128
+    packed, exps, W, F = make_layer(q, N, K, G)
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    xs = [torch.randn((r, K), device="cuda", generator=gen(r)).half() for r in (5, 500)]
+    ys = [torch.empty((x.shape[0], N), device="cuda") for x in xs]
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for st, x, y in zip(streams, xs, ys):
+            sa.sa_shiftadd_gemm_epilogue(x, packed, exps, q, N, K, G, x.shape[0], None, "silu", None,
+                                         None, y, stream=st)
+    torch.cuda.synchronize()
+    for x, y in zip(xs, ys):
+        check(y, *expected(x, W[0], F[0], q, None, "silu", None, None, 0), "two streams")
+
+
 # ------------------------------------------------------------------ experts
 
 def run_experts(q, N, K, G, counts, tokens, gather, act, bias, mul, half, lead=0, tail=0, seed=0,
@@ -307,6 +385,16 @@ def test_experts(counts, gather):
         run_experts(q, N, K, G, counts, tokens=max(sum(counts), 7), gather=gather,
                     act=ACTS[(i + len(counts)) % 5], bias=i % 2, mul=(i + gather) % 2,
                     half=(i + len(counts)) % 2, lead=3 * (i % 2), tail=5 * (i // 2), seed=i)
+
+
+def test_most_experts():
+    counts = [(7 * e) % 5 for e in range(sa.SA_MAX_EXPERTS)]
+    run_experts(2, 16, 128, 128, counts, 50, 1, "silu", 1, 1, 1, lead=2, tail=3)
+
+
+@pytest.mark.parametrize("q,K,G", [(7, 256, 128), (6, 384, 128), (8, 192, 32), (4, 320, 16)])
+def test_experts_of_many_planes(q, K, G):
+    run_experts(q, 70, K, G, [3, 0, 70, 9], 60, 1, "relu", 1, 0, 0)
 
 
 @pytest.mark.parametrize("counts", [[3, 0, 12], [100, 40, 0, 5]])
