@@ -795,6 +795,7 @@ void k_panel(Args pa) {
     if constexpr (CT == 8) {
         if (rows <= 2 * kTile) return body<Q, 2, KW, GEN>(pa, xbuf, expert, first, end);
         if (rows <= 4 * kTile) return body<Q, 4, KW, GEN>(pa, xbuf, expert, first, end);
+        if (rows <= 6 * kTile) return body<Q, 6, KW, GEN>(pa, xbuf, expert, first, end);
     } else if constexpr (CT == 4 || (CT == 2 && KW > 1)) {
         if (rows <= CT / 2 * kTile) return body<Q, CT / 2, KW, GEN>(pa, xbuf, expert, first, end);
     }

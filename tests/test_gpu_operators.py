@@ -155,6 +155,17 @@ def test_epilogue_exponent_ranges(rows, lo, hi):
         run_epilogue(q, N, K, G, rows, "none", 0, 0, 0, 0, lo, hi)
 
 
+# sizes at which each tile shape of the panel kernel has the least estimate, with rows that
+# end inside a tile: 256 rows; 128 with and without column shares; 64; 32
+@pytest.mark.parametrize("q", [1, 2, 3, 4, 5, 8])
+@pytest.mark.parametrize("N,K,rows", [(4096, 4096, 4010), (4096, 1024, 1200), (4096, 1024, 600),
+                                      (2048, 512, 700), (2048, 1024, 300), (512, 2048, 200),
+                                      (1024, 1024, 100)])
+def test_epilogue_tile_shapes(N, K, rows, q):
+    for lo, hi in ((-8, -2), (-20, 3)):   # planes summed; some blocks plane by plane
+        run_epilogue(q, N, K, 128, rows, "silu", 1, 1, 1, q % 2, lo, hi)
+
+
 def test_epilogue_extreme_exponents():
     """Factors near the ends of fp32's range."""
     q, N, K, G = 2, 64, 256, 128
@@ -385,6 +396,12 @@ def test_experts(counts, gather):
         run_experts(q, N, K, G, counts, tokens=max(sum(counts), 7), gather=gather,
                     act=ACTS[(i + len(counts)) % 5], bias=i % 2, mul=(i + gather) % 2,
                     half=(i + len(counts)) % 2, lead=3 * (i % 2), tail=5 * (i // 2), seed=i)
+
+
+@pytest.mark.parametrize("q", [1, 2, 3, 4])
+def test_experts_tile_heights(q):
+    """Tiles of 256 rows that end after 40, 100, 170 and 250 rows."""
+    run_experts(q, 8192, 2048, 128, [296, 356, 426, 762], 500, 1, "silu", 1, 1, q % 2, tail=3)
 
 
 def test_most_experts():
