@@ -45,6 +45,7 @@ typedef float float16_t __attribute__((ext_vector_type(16)));
 constexpr int kWaves = 8;
 constexpr int kThreads = 64 * kWaves;
 constexpr int kTile = 32;  // outputs and rows of one matrix tile
+constexpr int kFarWords = 128;
 
 struct Args {
     Layer a;
@@ -147,7 +148,8 @@ struct Keys {
 // a block are 256 bytes of LDS, chunk c at 16 (c ^ (row & 15)): both the copies (whole
 // rows) and the reads (16 lanes at a time, one step) touch every bank once.
 template <int Q, int CT, int KW, int GEN>
-__device__ __forceinline__ void body(const Args& pa, uint4* xbuf, int expert, int first, int end) {
+__device__ __forceinline__ void body(const Args& pa, uint4* xbuf, uint32_t* far_steps, int expert,
+                                     int first, int end) {
     const Layer& a = pa.a;
     constexpr int RW = kWaves / KW;
     constexpr int kItems = CT * 8 / RW;  // 1 KiB copies (4 rows) of a wave a block
@@ -595,8 +597,16 @@ __device__ __forceinline__ void body(const Args& pa, uint4* xbuf, int expert, in
         return far;
     };
 
+    // Blocks left for the second loop, a bit per two steps (steps far apart share one): it
+    // visits those alone (11008x4096, 250 rows: 41 us, one such group in the layer 55, which
+    // took 79 over all blocks; every block 194).
+    bool left = false;
+    auto leave = [&](int s) {
+        left = true;
+        if (lane == 0) atomicOr(&far_steps[(s >> 6) & (kFarWords - 1)], 1u << ((s >> 1) & 31));
+    };
+    if ((int)threadIdx.x < kFarWords) far_steps[threadIdx.x] = 0u;
     Keys<Q, GEN> k;
-    bool left = false;  // blocks were left for the second loop
     if (blk0 < blk1) {
         copy_x(blk0, 0);
         load_keys(blk0, k);
@@ -611,7 +621,7 @@ __device__ __forceinline__ void body(const Args& pa, uint4* xbuf, int expert, in
                 const Keys<Q, GEN> now = GEN == kPart ? spread_out(k, J) : k;
                 if (J + 1 < blk1) load_keys(J + 1, k);
                 if (__any(block_far(now)))
-                    left = true;
+                    leave(s);
                 else
                     summed(J, xr + (s & 1) * kBuf,
                            [&](int i, int h) { return word_of(now, i, h); },
@@ -625,7 +635,7 @@ __device__ __forceinline__ void body(const Args& pa, uint4* xbuf, int expert, in
         for (int s0 = 0; s0 < steps; s0 += 2) {
             uint32_t wd[2][Q][2], ew[2][kE];
             const bool far = __any(unpack(k, wd, ew) && blk0 + s0 + g < blk1);
-            left |= far;
+            if (far) leave(s0);
             const int J0 = blk0 + s0;
             auto e0 = [&](int i, int) { return (int)(int8_t)(ew[0][i >> 2] >> (8 * (i & 3))); };
             auto e1 = [&](int i, int) { return (int)(int8_t)(ew[1][i >> 2] >> (8 * (i & 3))); };
@@ -686,6 +696,9 @@ __device__ __forceinline__ void body(const Args& pa, uint4* xbuf, int expert, in
     if (__syncthreads_or(left)) {
 #pragma unroll 1
         for (int s = 0; s < steps; ++s) {
+            const uint32_t word = (uint32_t)__builtin_amdgcn_readfirstlane(
+                (int)far_steps[(s >> 6) & (kFarWords - 1)]);
+            if (!(word >> ((s >> 1) & 31) & 1u)) continue;  // uniform over the workgroup
             const int J = blk0 + s;
             if (J < blk1) copy_x(J, 0);
             arrive();
@@ -786,6 +799,7 @@ template <int Q, int CT, int KW, int GEN>
 __global__ __launch_bounds__(kThreads, CT == 1 && Q <= 4 && !GEN ? 4 : 2)
 void k_panel(Args pa) {
     __shared__ uint4 xbuf[KW * 2 * CT * 512];
+    __shared__ uint32_t far_steps[kFarWords];
     int expert, first, end;
     if (!sa_linear::find_tile(pa.a, kTile * CT, (int)(blockIdx.x / (unsigned)pa.n_tiles), &expert,
                               &first, &end))
@@ -793,13 +807,13 @@ void k_panel(Args pa) {
     // a tile of fewer rows runs the body of their height
     const int rows = end - first;
     if constexpr (CT == 8) {
-        if (rows <= 2 * kTile) return body<Q, 2, KW, GEN>(pa, xbuf, expert, first, end);
-        if (rows <= 4 * kTile) return body<Q, 4, KW, GEN>(pa, xbuf, expert, first, end);
-        if (rows <= 6 * kTile) return body<Q, 6, KW, GEN>(pa, xbuf, expert, first, end);
+        if (rows <= 2 * kTile) return body<Q, 2, KW, GEN>(pa, xbuf, far_steps, expert, first, end);
+        if (rows <= 4 * kTile) return body<Q, 4, KW, GEN>(pa, xbuf, far_steps, expert, first, end);
+        if (rows <= 6 * kTile) return body<Q, 6, KW, GEN>(pa, xbuf, far_steps, expert, first, end);
     } else if constexpr (CT == 4 || (CT == 2 && KW > 1)) {
-        if (rows <= CT / 2 * kTile) return body<Q, CT / 2, KW, GEN>(pa, xbuf, expert, first, end);
+        if (rows <= CT / 2 * kTile) return body<Q, CT / 2, KW, GEN>(pa, xbuf, far_steps, expert, first, end);
     }
-    body<Q, CT, KW, GEN>(pa, xbuf, expert, first, end);
+    body<Q, CT, KW, GEN>(pa, xbuf, far_steps, expert, first, end);
 }
 
 template <int Q, int CT, int KW, int GEN>
