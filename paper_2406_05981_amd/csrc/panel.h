@@ -437,61 +437,103 @@ __device__ __forceinline__ void body(const Args& pa, uint4* xbuf, uint32_t* far_
     };
 
     // Any exponents: a product a plane in bfloat16, whose range holds +-2^e, with the
-    // activations as two exact pieces.
-    auto plane_by_plane = [&](int J, const uint4* xs, auto w, auto e) {
+    // activations as two exact pieces.  A group's sum may be finite where a factor times one
+    // activation is not: factors above 2^kTop have their block's sum apart, at 2^-kTopShift.
+    constexpr int kTop = 100, kTopShift = 64;
+    struct Planes {
         uint64_t keys[Q], ex[Q];  // a byte per step, the next one lowest
+    };
+    auto planes_of = [&](auto w, auto e) {
+        Planes p;
 #pragma unroll
         for (int i = 0; i < Q; ++i) {
-            keys[i] = (uint64_t)w(i, 1) << 32 | w(i, 0);
-            ex[i] = 0;
+            p.keys[i] = (uint64_t)w(i, 1) << 32 | w(i, 0);
+            p.ex[i] = 0;
 #pragma unroll
             for (int s = 0; s < (GEN ? 8 : 1); ++s)
-                ex[i] |= (uint64_t)(uint8_t)e(i, s) << (8 * s);
+                p.ex[i] |= (uint64_t)(uint8_t)e(i, s) << (8 * s);
         }
+        return p;
+    };
+    // The planes' operands of step s; `apart`: those above kTop alone, else the others alone.
+    auto next_step = [&](int J, int s, bool apart, Planes& p, bhalf8_t (&W)[Q]) {
+#pragma unroll
+        for (int i = 0; i < Q; ++i) {
+            const Spread sp = spread((uint32_t)p.keys[i], 0);
+            const int own = (int)(int8_t)p.ex[i], ei = apart ? own - kTopShift : own;
+            // 2^-127 and 2^-128 are subnormal
+            uint32_t mag = ei > -127 ? (uint32_t)(ei + 127) << 7 : ei == -127 ? 0x40u : 0x20u;
+            mag |= mag << 16;
+            const bool none = i >= a.q || !inside(J, s) || (own > kTop) != apart;
+            uint32_t v[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                v[j] = none ? 0u : ((sp.v << (15 - 2 * j)) & 0x80008000u) ^ (mag | 0x80008000u);
+            W[i] = __builtin_bit_cast(bhalf8_t, uint4{v[0], v[1], v[2], v[3]});
+            p.keys[i] >>= 8;
+            if constexpr (GEN) p.ex[i] >>= 8;
+        }
+    };
+    auto add_planes = [&](const uint4* xs, int s, int c, const bhalf8_t (&W)[Q], float16_t sum) {
+        const half8_t X = __builtin_bit_cast(half8_t, xs[512 * c + ((2 * s) ^ x_word)]);
+        uint32_t hi[4], lo[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            // eight significant bits, and the at most three behind them
+            const float f0 = (float)X[2 * j], f1 = (float)X[2 * j + 1];
+            const uint32_t h0 = __builtin_bit_cast(uint32_t, f0) & 0xffff0000u;
+            const uint32_t h1 = __builtin_bit_cast(uint32_t, f1) & 0xffff0000u;
+            const float l0 = f0 - __builtin_bit_cast(float, h0);
+            const float l1 = f1 - __builtin_bit_cast(float, h1);
+            hi[j] = h0 >> 16 | h1;
+            lo[j] = __builtin_bit_cast(uint32_t, l0) >> 16 |
+                    (__builtin_bit_cast(uint32_t, l1) & 0xffff0000u);
+        }
+        const bhalf8_t H = __builtin_bit_cast(bhalf8_t, uint4{hi[0], hi[1], hi[2], hi[3]});
+        const bhalf8_t L = __builtin_bit_cast(bhalf8_t, uint4{lo[0], lo[1], lo[2], lo[3]});
+#pragma unroll
+        for (int i = 0; i < Q; ++i) {
+            sum = __builtin_amdgcn_mfma_f32_32x32x16_bf16(W[i], H, sum, 0, 0, 0);
+            sum = __builtin_amdgcn_mfma_f32_32x32x16_bf16(W[i], L, sum, 0, 0, 0);
+        }
+        return sum;
+    };
+    auto plane_by_plane = [&](int J, const uint4* xs, auto w, auto e) {
+        Planes p = planes_of(w, e);
+        bool top = false;
+#pragma unroll
+        for (int i = 0; i < Q; ++i)
+#pragma unroll
+            for (int s = 0; s < (GEN ? 8 : 1); ++s) top |= e(i, s) > kTop;
 #pragma unroll 1
         for (int s = 0; s < 8; ++s) {
             bhalf8_t W[Q];
-#pragma unroll
-            for (int i = 0; i < Q; ++i) {
-                const Spread sp = spread((uint32_t)keys[i], 0);
-                const int ei = (int)(int8_t)ex[i];
-                // 2^-127 and 2^-128 are subnormal
-                uint32_t mag = ei > -127 ? (uint32_t)(ei + 127) << 7 : ei == -127 ? 0x40u : 0x20u;
-                mag |= mag << 16;
-                const bool none = i >= a.q || !inside(J, s);
-                uint32_t p[4];
-#pragma unroll
-                for (int j = 0; j < 4; ++j)
-                    p[j] = none ? 0u : ((sp.v << (15 - 2 * j)) & 0x80008000u) ^ (mag | 0x80008000u);
-                W[i] = __builtin_bit_cast(bhalf8_t, uint4{p[0], p[1], p[2], p[3]});
-                keys[i] >>= 8;
-                if constexpr (GEN) ex[i] >>= 8;
-            }
+            next_step(J, s, false, p, W);
 #pragma unroll
             for (int c = 0; c < CT; ++c) {
-                const half8_t X = __builtin_bit_cast(half8_t, xs[512 * c + ((2 * s) ^ x_word)]);
-                uint32_t hi[4], lo[4];
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    // eight significant bits, and the at most three behind them
-                    const float f0 = (float)X[2 * j], f1 = (float)X[2 * j + 1];
-                    const uint32_t h0 = __builtin_bit_cast(uint32_t, f0) & 0xffff0000u;
-                    const uint32_t h1 = __builtin_bit_cast(uint32_t, f1) & 0xffff0000u;
-                    const float l0 = f0 - __builtin_bit_cast(float, h0);
-                    const float l1 = f1 - __builtin_bit_cast(float, h1);
-                    hi[j] = h0 >> 16 | h1;
-                    lo[j] = __builtin_bit_cast(uint32_t, l0) >> 16 |
-                            (__builtin_bit_cast(uint32_t, l1) & 0xffff0000u);
-                }
-                const bhalf8_t H = __builtin_bit_cast(bhalf8_t, uint4{hi[0], hi[1], hi[2], hi[3]});
-                const bhalf8_t L = __builtin_bit_cast(bhalf8_t, uint4{lo[0], lo[1], lo[2], lo[3]});
-#pragma unroll
-                for (int i = 0; i < Q; ++i) {
-                    acc[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(W[i], H, acc[c], 0, 0, 0);
-                    acc[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(W[i], L, acc[c], 0, 0, 0);
-                }
+                acc[c] = add_planes(xs, s, c, W, acc[c]);
                 __builtin_amdgcn_sched_barrier(0);
             }
+        }
+        if (!__any(top)) return;
+        // (not unrolled: the row tiles take turns in acc[0], and no registers are added)
+#pragma unroll 1
+        for (int c = 0; c < CT; ++c) {
+            p = planes_of(w, e);
+            float16_t sum;
+#pragma unroll
+            for (int v = 0; v < 16; ++v) sum[v] = 0.0f;
+#pragma unroll 1
+            for (int s = 0; s < 8; ++s) {
+                bhalf8_t W[Q];
+                next_step(J, s, true, p, W);
+                sum = add_planes(xs, s, c, W, sum);
+            }
+#pragma unroll
+            for (int v = 0; v < 16; ++v) sum[v] = acc[0][v] + ldexpf(sum[v], kTopShift);
+#pragma unroll
+            for (int i = 0; i + 1 < CT; ++i) acc[i] = acc[i + 1];
+            acc[CT - 1] = sum;
         }
     };
 
