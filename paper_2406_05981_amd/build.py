@@ -16,9 +16,9 @@ import sys
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 SOURCES = [os.path.join(HERE, "csrc", name)
-           for name in ("shiftadd.hip", "gemm_mx.hip", "gemm_mfma.hip", "linear.hip", "panel.hip",
-                        "panel_groups.hip", "route.hip",
-                        "bcq.hip", "alloc.hip")]
+           for name in ("shiftadd.hip", "panel_groups.hip", "panel.hip", "panel_planes.hip",
+                        "panel_chunks.hip", "gemm_mx.hip", "gemm_mfma.hip", "linear.hip",
+                        "route.hip", "bcq.hip", "alloc.hip")]
 INCLUDE = os.path.join(ROOT, "include")
 HEADERS = [os.path.join(INCLUDE, "shiftadd.h")] + [
     os.path.join(HERE, "csrc", name)

@@ -892,6 +892,20 @@ void start_form(Args& pa, const Form& f, hipStream_t s) {
     }
 }
 
+// The arguments of a layer whose groups are whole blocks, and of any other.
+inline Args other_args(const Layer& a) {
+    Args pa{};
+    pa.a = a;
+    pa.byte_offsets = (int64_t)a.x_rows * a.K < (int64_t)1 << 31;
+    return pa;
+}
+inline Args whole_args(const Layer& a) {
+    Args pa = other_args(a);
+    const uint32_t d = (uint32_t)(a.G / 128);
+    pa.group_magic = d <= 1 ? 0u : (uint32_t)(((1ull << 32) + d - 1) / d);
+    return pa;
+}
+
 }  // namespace
 }  // namespace sa_panel
 

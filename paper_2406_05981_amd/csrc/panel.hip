@@ -6,6 +6,8 @@ namespace sa_panel {
 
 // panel_groups.hip
 void launch_groups(const sa_linear::Layer& a, int ct, int kw, hipStream_t s);
+// panel_planes.hip
+void launch_planes(const sa_linear::Layer& a, int ct, int kw, hipStream_t s);
 
 namespace {
 
@@ -70,19 +72,15 @@ void launch(const Layer& a, hipStream_t s) {
         launch_groups(a, f->ct, f->kw, s);
         return;
     }
-    Args pa{};
-    pa.a = a;
-    const uint32_t d = (uint32_t)(a.G / 128);
-    pa.group_magic = d <= 1 ? 0u : (uint32_t)(((1ull << 32) + d - 1) / d);
-    pa.byte_offsets = (int64_t)a.x_rows * a.K < (int64_t)1 << 31;
+    if (a.q > 3) {
+        launch_planes(a, f->ct, f->kw, s);
+        return;
+    }
+    Args pa = whole_args(a);
     switch (a.q) {
         case 1: start_form<1, kWhole>(pa, *f, s); break;
         case 2: start_form<2, kWhole>(pa, *f, s); break;
-        case 3: start_form<3, kWhole>(pa, *f, s); break;
-        case 4: start_form<4, kWhole>(pa, *f, s); break;
-        case 5:
-        case 6: start_form<6, kWhole>(pa, *f, s); break;
-        default: start_form<8, kWhole>(pa, *f, s); break;
+        default: start_form<3, kWhole>(pa, *f, s); break;
     }
 }
 
