@@ -519,6 +519,31 @@ def sa_read_probe(buf: torch.Tensor, nbytes: int, out: torch.Tensor, stream=None
 
 
 # ------------------------------------------------------------------ conveniences
+#
+# `stream`: the call runs there, in the order of its work (None: the current stream).  The
+# caller sees to it that the inputs are ready on it and live until it is done with them.
+
+def _other(stream) -> Optional[torch.cuda.Stream]:
+    """``stream`` as a torch stream, or None if it is the current one."""
+    if stream is None or _stream(stream) == _stream(None):
+        return None
+    return stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(
+        int(stream))
+
+
+def _run_on(other: torch.cuda.Stream, f, *args):
+    """``f(*args)`` with ``other`` as the current stream: what it allocates belongs to the
+    stream that writes it, so a temporary freed here is not handed to work elsewhere while
+    ``other`` still uses it, nor the other way round.  What is returned is used on the
+    caller's stream: freed, it waits for that one too."""
+    caller = torch.cuda.current_stream()
+    with torch.cuda.stream(other):
+        result = f(*args)
+    for t in result if isinstance(result, tuple) else (result,):
+        if isinstance(t, torch.Tensor):
+            t.record_stream(caller)
+    return result
+
 
 def quantize_bcq(w: torch.Tensor, q: int, group: int, cycles: int, stream=None):
     """``(signs int8 [q][N][K], exps int8 [q][N][K/group])`` of fp32 weights
@@ -590,6 +615,10 @@ def shiftadd_linear(x: torch.Tensor, packed_bits: torch.Tensor, exps: torch.Tens
                     stream=None) -> torch.Tensor:
     """``activation(x W_q^T + bias) * multiplier + residual`` of any number of rows as a new
     (or the given) ``[rows][N]`` tensor."""
+    other = _other(stream) if out is None else None
+    if other is not None:
+        return _run_on(other, shiftadd_linear, x, packed_bits, exps, q, N, K, group, bias,
+                       activation, multiplier, residual, out_dtype)
     rows = x.numel() // K
     y = out if out is not None else torch.empty((rows, N), dtype=out_dtype, device=x.device)
     sa_shiftadd_gemm_epilogue(x, packed_bits, exps, q, N, K, group, rows, bias, activation,
@@ -600,6 +629,9 @@ def shiftadd_linear(x: torch.Tensor, packed_bits: torch.Tensor, exps: torch.Tens
 def route_experts(logits: torch.Tensor, k: int, normalize: bool = True, stream=None):
     """``(ids, weights, offsets, row_of, slot_of)`` of fp32 router logits
     ``[tokens][experts]`` (new device tensors)."""
+    other = _other(stream)
+    if other is not None:
+        return _run_on(other, route_experts, logits, k, normalize)
     tokens, experts = logits.shape
     new = lambda *shape: torch.empty(shape, dtype=torch.int32, device=logits.device)  # noqa: E731
     ids, slot_of, row_of, offsets = new(tokens, k), new(tokens, k), new(tokens * k), new(experts + 1)
@@ -618,6 +650,10 @@ def shiftadd_moe(x: torch.Tensor, logits: torch.Tensor, k: int, gate, up, down, 
     each token's ``k`` experts, as a new fp16 ``[tokens][K]`` tensor.  ``gate``, ``up`` (N x K
     layers) and ``down`` (K x N) are ``(packed_bits, exps, q)`` of all experts; ``logits`` fp32
     ``[tokens][experts]``."""
+    other = _other(stream)
+    if other is not None:
+        return _run_on(other, shiftadd_moe, x, logits, k, gate, up, down, N, K, group, residual,
+                       normalize)
     tokens, experts = logits.shape
     slots = tokens * k
     _, weights, offsets, row_of, slot_of = route_experts(logits, k, normalize, stream)
