@@ -548,6 +548,9 @@ def _run_on(other: torch.cuda.Stream, f, *args):
 def quantize_bcq(w: torch.Tensor, q: int, group: int, cycles: int, stream=None):
     """``(signs int8 [q][N][K], exps int8 [q][N][K/group])`` of fp32 weights
     ``[N][K]`` (new device tensors), in the layer's format."""
+    other = _other(stream)
+    if other is not None:
+        return _run_on(other, quantize_bcq, w, q, group, cycles)
     N, K = w.shape
     signs = torch.empty((q, N, K), dtype=torch.int8, device=w.device)
     exps = torch.empty((q, N, K // group), dtype=torch.int8, device=w.device)
@@ -559,6 +562,9 @@ def quantize_bcq_terms(w: torch.Tensor, q: int, group: int, cycles: int, terms: 
                        stream=None):
     """``(signs [q][N][K], exps [q][N][K/group][terms], term_signs [q][N][K/group][terms])``
     (int8, new device tensors) with additive PoT scales."""
+    other = _other(stream)
+    if other is not None:
+        return _run_on(other, quantize_bcq_terms, w, q, group, cycles, terms)
     N, K = w.shape
     signs = torch.empty((q, N, K), dtype=torch.int8, device=w.device)
     exps = torch.empty((q, N, K // group, terms), dtype=torch.int8, device=w.device)
@@ -569,6 +575,9 @@ def quantize_bcq_terms(w: torch.Tensor, q: int, group: int, cycles: int, terms: 
 
 def pack_weights(signs: torch.Tensor, stream=None) -> torch.Tensor:
     """Packed planes of ``int8 [q][N][K]`` signs (a new uint8 device tensor)."""
+    other = _other(stream)
+    if other is not None:
+        return _run_on(other, pack_weights, signs)
     q, N, K = signs.shape
     packed = torch.empty(sa_packed_bytes(q, N, K), dtype=torch.uint8, device=signs.device)
     sa_pack_weights(signs, q, N, K, packed, stream)
@@ -579,6 +588,9 @@ def shiftadd_gemm(x: torch.Tensor, packed_bits: torch.Tensor, exps: torch.Tensor
                   K: int, group: int, out: Optional[torch.Tensor] = None,
                   stream=None) -> torch.Tensor:
     """``y = x W_q^T`` as a new (or the given) fp32 ``[batch][N]`` tensor."""
+    other = _other(stream) if out is None else None
+    if other is not None:
+        return _run_on(other, shiftadd_gemm, x, packed_bits, exps, q, N, K, group)
     batch = x.shape[0] if x.dim() == 2 else 1
     y = out if out is not None else torch.empty((batch, N), dtype=torch.float32, device=x.device)
     sa_shiftadd_gemm(x, packed_bits, exps, q, N, K, group, batch, y, stream)
@@ -590,6 +602,9 @@ def shiftadd_gemm_colwise(x: torch.Tensor, packed_bits: torch.Tensor, col_exps: 
                           stream=None) -> torch.Tensor:
     """``y = x W_q^T`` with column-wise factors, as a new (or the given) fp32
     ``[batch][N]`` tensor."""
+    other = _other(stream) if out is None else None
+    if other is not None:
+        return _run_on(other, shiftadd_gemm_colwise, x, packed_bits, col_exps, q, N, K)
     batch = x.shape[0] if x.dim() == 2 else 1
     y = out if out is not None else torch.empty((batch, N), dtype=torch.float32, device=x.device)
     sa_shiftadd_gemm_colwise(x, packed_bits, col_exps, q, N, K, batch, y, stream)
@@ -601,6 +616,9 @@ def shiftadd_gemm_blockwise(x: torch.Tensor, packed_bits: torch.Tensor, blk_exps
                             out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """``y = x W_q^T`` with block-wise factors, as a new (or the given) fp32
     ``[batch][N]`` tensor."""
+    other = _other(stream) if out is None else None
+    if other is not None:
+        return _run_on(other, shiftadd_gemm_blockwise, x, packed_bits, blk_exps, q, N, K, row_block)
     batch = x.shape[0] if x.dim() == 2 else 1
     y = out if out is not None else torch.empty((batch, N), dtype=torch.float32, device=x.device)
     sa_shiftadd_gemm_blockwise(x, packed_bits, blk_exps, q, N, K, row_block, batch, y, stream)
@@ -674,6 +692,9 @@ def bit_criterion(w: torch.Tensor, x: torch.Tensor, damp: float = 0.01, stream=N
     """Eq. 3 for one layer: ``(C, ||IS||_F, STD(IS), d)`` from fp32 weights
     ``[N][K]`` and fp16 calibration activations ``[K][T]`` on the device
     (workspaces are new device tensors)."""
+    other = _other(stream)
+    if other is not None:
+        return _run_on(other, bit_criterion, w, x, damp)
     N, K = w.shape
     T = x.shape[1]
     H = torch.empty((K, K), dtype=torch.float32, device=w.device)

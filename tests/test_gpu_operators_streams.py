@@ -66,3 +66,27 @@ def test_linear_and_router_on_a_side_stream():
     torch.cuda.synchronize()
     assert torch.equal(y, want) and torch.equal(given, want)
     assert all(torch.equal(a, b) for a, b in zip(r, routed))
+
+
+def test_layer_and_quantizer_on_a_side_stream():
+    q, N, K, G, rows = 2, 100, 512, 128, 12
+    w = torch.randn((N, K), device="cuda", generator=gen(3))
+    x = torch.randn((rows, K), device="cuda", generator=gen(4)).half()
+    calib = torch.randn((K, 1024), device="cuda", generator=gen(5)).half()
+    signs, exps = sa.quantize_bcq(w, q, G, 5)
+    packed = sa.pack_weights(signs)
+    want = sa.shiftadd_gemm(x, packed, exps, q, N, K, G)
+    criterion = sa.bit_criterion(w, calib)
+    side = torch.cuda.Stream()
+    busy(side)
+    s, e = sa.quantize_bcq(w, q, G, 5, stream=side)
+    p = sa.pack_weights(s, stream=side)
+    y = sa.shiftadd_gemm(x, p, e, q, N, K, G, stream=side)
+    torch.cuda.synchronize()
+    assert torch.equal(s, signs) and torch.equal(e, exps) and torch.equal(p, packed)
+    assert torch.equal(y, want)
+    busy(side)
+    c = sa.bit_criterion(w, calib, stream=side)
+    assert c[:3] == criterion[:3]
+    torch.cuda.synchronize()
+    assert torch.equal(c[3], criterion[3])

@@ -22,9 +22,16 @@ class Tensor(torch.Tensor):
     def record_stream(self, stream):
         self.recorded = getattr(self, "recorded", []) + [stream.cuda_stream]
 
+    def cpu(self):
+        World.read_on.append(torch.cuda.current_stream().cuda_stream)
+        return self.zero_()
+
 
 class World:
+    read_on = []   # stream of every copy to the host
+
     def __init__(self, monkeypatch):
+        World.read_on.clear()
         self.current = Stream(CALLER)
         self.allocated = []   # stream of every allocation
         self.calls = []       # stream of every library call
@@ -56,7 +63,10 @@ class World:
             monkeypatch.setattr(sa.lib, name, call)
 
     LIBRARY = ("sa_shiftadd_gemm_epilogue", "sa_shiftadd_gemm_experts", "sa_route_experts",
-               "sa_combine_experts")
+               "sa_combine_experts", "sa_pack_weights", "sa_shiftadd_gemm",
+               "sa_shiftadd_gemm_colwise", "sa_shiftadd_gemm_blockwise", "sa_quantize_bcq",
+               "sa_quantize_bcq_terms", "sa_gram_f16", "sa_inverse_cholesky_diag",
+               "sa_importance_criterion")
 
 
 @pytest.fixture
@@ -79,7 +89,42 @@ def moe(**kw):
                            256, 128, 128, **kw)
 
 
-@pytest.mark.parametrize("f", [linear, route, moe])
+def pack(**kw):
+    return sa.pack_weights(torch.zeros(1, 16, 128).char(), **kw)
+
+
+def plain(out=None, **kw):
+    return sa.shiftadd_gemm(torch.zeros(2, 128).half(), torch.zeros(8), torch.zeros(8), 1, 16, 128,
+                            128, out=out, **kw)
+
+
+def colwise(out=None, **kw):
+    return sa.shiftadd_gemm_colwise(torch.zeros(2, 128).half(), torch.zeros(8), torch.zeros(8), 1, 16,
+                                    128, out=out, **kw)
+
+
+def blockwise(out=None, **kw):
+    return sa.shiftadd_gemm_blockwise(torch.zeros(2, 128).half(), torch.zeros(8), torch.zeros(8), 1,
+                                      16, 128, 2, out=out, **kw)
+
+
+def quantize(**kw):
+    return sa.quantize_bcq(torch.zeros(16, 128), 2, 128, 3, **kw)
+
+
+def quantize_terms(**kw):
+    return sa.quantize_bcq_terms(torch.zeros(16, 128), 2, 128, 3, 2, **kw)
+
+
+def criterion(**kw):
+    return sa.bit_criterion(torch.zeros(16, 128), torch.zeros(128, 64).half(), **kw)[3:]
+
+
+CONVENIENCES = [linear, route, moe, pack, plain, colwise, blockwise, quantize, quantize_terms,
+                criterion]
+
+
+@pytest.mark.parametrize("f", CONVENIENCES)
 def test_memory_belongs_to_the_stream_that_writes_it(world, f):
     """Temporaries freed while the stream's work is queued go back to that stream alone, and no
     block that the caller's stream still uses is written; what is returned waits for the caller's
@@ -92,7 +137,7 @@ def test_memory_belongs_to_the_stream_that_writes_it(world, f):
         assert CALLER in t.recorded
 
 
-@pytest.mark.parametrize("f", [linear, route, moe])
+@pytest.mark.parametrize("f", CONVENIENCES)
 @pytest.mark.parametrize("kw", [{}, {"stream": CALLER}])
 def test_the_current_stream_needs_nothing(world, f, kw):
     out = f(**kw)
@@ -101,7 +146,13 @@ def test_the_current_stream_needs_nothing(world, f, kw):
         assert not hasattr(t, "recorded")
 
 
-def test_a_given_output_is_the_callers(world):
+@pytest.mark.parametrize("f", [linear, plain, colwise, blockwise])
+def test_a_given_output_is_the_callers(world, f):
     y = torch.zeros(3, 16).half()
-    assert linear(out=y, stream=SIDE) is y
+    assert f(out=y, stream=SIDE) is y
     assert world.allocated == [] and world.calls == [SIDE]
+
+
+def test_the_criterion_is_read_on_its_stream(world):
+    sa.bit_criterion(torch.zeros(16, 128), torch.zeros(128, 64).half(), stream=SIDE)
+    assert World.read_on == [SIDE]
