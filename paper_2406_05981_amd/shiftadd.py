@@ -124,23 +124,35 @@ _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
 _current_device = getattr(torch._C, "_cuda_getDevice", None)
 
 
-def _stream(stream) -> int:
+def _stream(stream, here: Optional[int] = None) -> int:
     if stream is None:
+        if here is not None and _raw_stream is not None:
+            return _raw_stream(here)
         if _raw_stream is not None and _current_device is not None and torch.cuda.is_initialized():
             return _raw_stream(_current_device())
         return torch.cuda.current_stream().cuda_stream
     if isinstance(stream, torch.cuda.Stream):
+        if here is not None and stream.device_index != here:
+            raise ValueError(f"stream must be of the current device, cuda:{here}")
         return stream.cuda_stream
     return int(stream)
 
 
-def _dev(t: torch.Tensor, name: str, dtype: torch.dtype, numel: int) -> int:
+# The current device, where a call's kernels run and its tensors have to be.
+_here = _current_device or torch.cuda.current_device
+
+
+def _dev(t: torch.Tensor, name: str, dtype: torch.dtype, numel: int,
+         here: Optional[int] = None) -> int:
     if not isinstance(t, torch.Tensor):
         raise TypeError(f"{name} must be a torch.Tensor")
-    if t.dtype == dtype and t.is_cuda and t.numel() == numel and t.is_contiguous():
+    if (t.dtype == dtype and (t.is_cuda if here is None else t.get_device() == here)
+            and t.numel() == numel and t.is_contiguous()):
         return t.data_ptr()
     if not t.is_cuda:
         raise ValueError(f"{name} must be on the GPU")
+    if here is not None and t.get_device() != here:
+        raise ValueError(f"{name} must be on the current device, cuda:{here}")
     if t.dtype != dtype:
         raise ValueError(f"{name} must be {dtype}, got {t.dtype}")
     if not t.is_contiguous():
@@ -148,8 +160,9 @@ def _dev(t: torch.Tensor, name: str, dtype: torch.dtype, numel: int) -> int:
     raise ValueError(f"{name} must have {numel} elements, got {t.numel()}")
 
 
-def _opt(t: Optional[torch.Tensor], name: str, dtype: torch.dtype, numel: int) -> Optional[int]:
-    return None if t is None else _dev(t, name, dtype, numel)
+def _opt(t: Optional[torch.Tensor], name: str, dtype: torch.dtype, numel: int,
+         here: int) -> Optional[int]:
+    return None if t is None else _dev(t, name, dtype, numel, here)
 
 
 def _activation(name: str) -> int:
@@ -347,17 +360,19 @@ def sa_shiftadd_gemm_epilogue(x: torch.Tensor, packed_bits: torch.Tensor, exps: 
     """``y = activation(x W_q^T + bias) * multiplier + residual``; fp32 or binary16 by
     ``y``'s type, which ``multiplier`` and ``residual`` share."""
     nbytes = _layer_bytes(q, N, K, group, "sa_shiftadd_gemm_epilogue")
+    here = _here()
     half = _out_half(y)
     dtype, n = y.dtype, rows * N
     status = lib.sa_shiftadd_gemm_epilogue(
-        _dev(x, "x", torch.float16, rows * K),
-        _dev(packed_bits, "packed_bits", torch.uint8, nbytes),
-        _dev(exps, "exps", torch.int8, q * N * (K // group)),
+        _dev(x, "x", torch.float16, rows * K, here),
+        _dev(packed_bits, "packed_bits", torch.uint8, nbytes, here),
+        _dev(exps, "exps", torch.int8, q * N * (K // group), here),
         q, N, K, group, rows,
-        None if bias is None else _dev(bias, "bias", torch.float32, N), _activation(activation),
-        None if multiplier is None else _dev(multiplier, "multiplier", dtype, n),
-        None if residual is None else _dev(residual, "residual", dtype, n),
-        half, _dev(y, "y", dtype, n), _stream(stream))
+        None if bias is None else _dev(bias, "bias", torch.float32, N, here),
+        _activation(activation),
+        None if multiplier is None else _dev(multiplier, "multiplier", dtype, n, here),
+        None if residual is None else _dev(residual, "residual", dtype, n, here),
+        half, _dev(y, "y", dtype, n, here), _stream(stream, here))
     if status != SA_OK:
         _check(status, "sa_shiftadd_gemm_epilogue")
 
@@ -371,17 +386,19 @@ def sa_shiftadd_gemm_experts(x: torch.Tensor, row_of: Optional[torch.Tensor],
     """``y[s] = activation(x[row_of[s]] W_q^e^T + bias[e]) * multiplier[s]`` for the slots
     ``offsets[e] <= s < offsets[e + 1]`` of every expert e."""
     nbytes = _layer_bytes(q, N, K, group, "sa_shiftadd_gemm_experts")
+    here = _here()
     half = _out_half(y)
     x_rows = x.numel() // K if isinstance(x, torch.Tensor) else 0
     _check(lib.sa_shiftadd_gemm_experts(
-        _dev(x, "x", torch.float16, x_rows * K), x_rows,
-        _opt(row_of, "row_of", torch.int32, slots),
-        _dev(offsets, "offsets", torch.int32, experts + 1),
-        _dev(packed_bits, "packed_bits", torch.uint8, experts * nbytes),
-        _dev(exps, "exps", torch.int8, experts * q * N * (K // group)),
-        q, N, K, group, experts, slots, _opt(bias, "bias", torch.float32, experts * N),
-        _activation(activation), _opt(multiplier, "multiplier", y.dtype, slots * N),
-        half, _dev(y, "y", y.dtype, slots * N), _stream(stream)), "sa_shiftadd_gemm_experts")
+        _dev(x, "x", torch.float16, x_rows * K, here), x_rows,
+        _opt(row_of, "row_of", torch.int32, slots, here),
+        _dev(offsets, "offsets", torch.int32, experts + 1, here),
+        _dev(packed_bits, "packed_bits", torch.uint8, experts * nbytes, here),
+        _dev(exps, "exps", torch.int8, experts * q * N * (K // group), here),
+        q, N, K, group, experts, slots, _opt(bias, "bias", torch.float32, experts * N, here),
+        _activation(activation), _opt(multiplier, "multiplier", y.dtype, slots * N, here),
+        half, _dev(y, "y", y.dtype, slots * N, here), _stream(stream, here)),
+        "sa_shiftadd_gemm_experts")
 
 
 def sa_route_workspace_bytes(tokens: int, experts: int, k: int) -> int:
@@ -393,16 +410,17 @@ def sa_route_experts(logits: torch.Tensor, tokens: int, experts: int, k: int, no
                      row_of: torch.Tensor, slot_of: torch.Tensor,
                      workspace: Optional[torch.Tensor] = None, stream=None) -> None:
     nbytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    here = _here()
     _check(lib.sa_route_experts(
-        _dev(logits, "logits", torch.float32, tokens * experts), tokens, experts, k,
-        int(bool(normalize)), _dev(ids, "ids", torch.int32, tokens * k),
-        _dev(weights, "weights", torch.float32, tokens * k),
-        _dev(offsets, "offsets", torch.int32, experts + 1),
-        _dev(row_of, "row_of", torch.int32, tokens * k),
-        _dev(slot_of, "slot_of", torch.int32, tokens * k),
+        _dev(logits, "logits", torch.float32, tokens * experts, here), tokens, experts, k,
+        int(bool(normalize)), _dev(ids, "ids", torch.int32, tokens * k, here),
+        _dev(weights, "weights", torch.float32, tokens * k, here),
+        _dev(offsets, "offsets", torch.int32, experts + 1, here),
+        _dev(row_of, "row_of", torch.int32, tokens * k, here),
+        _dev(slot_of, "slot_of", torch.int32, tokens * k, here),
         None if workspace is None else _dev(workspace, "workspace", workspace.dtype,
-                                            workspace.numel()),
-        nbytes, _stream(stream)), "sa_route_experts")
+                                            workspace.numel(), here),
+        nbytes, _stream(stream, here)), "sa_route_experts")
 
 
 def sa_combine_experts(h: torch.Tensor, slot_of: torch.Tensor, weights: torch.Tensor, tokens: int,
@@ -414,11 +432,13 @@ def sa_combine_experts(h: torch.Tensor, slot_of: torch.Tensor, weights: torch.Te
     if N < 1:
         _check(SA_ERR_SHAPE, "sa_combine_experts")
     slots = h.numel() // N if isinstance(h, torch.Tensor) else 0
+    here = _here()
     _check(lib.sa_combine_experts(
-        _dev(h, "h", y.dtype, slots * N), _dev(slot_of, "slot_of", torch.int32, tokens * k),
-        _dev(weights, "weights", torch.float32, tokens * k), slots, tokens, k, N,
-        _opt(residual, "residual", y.dtype, tokens * N), half,
-        _dev(y, "y", y.dtype, tokens * N), _stream(stream)), "sa_combine_experts")
+        _dev(h, "h", y.dtype, slots * N, here),
+        _dev(slot_of, "slot_of", torch.int32, tokens * k, here),
+        _dev(weights, "weights", torch.float32, tokens * k, here), slots, tokens, k, N,
+        _opt(residual, "residual", y.dtype, tokens * N, here), half,
+        _dev(y, "y", y.dtype, tokens * N, here), _stream(stream, here)), "sa_combine_experts")
 
 
 def sa_quantize_bcq(w: torch.Tensor, N: int, K: int, q: int, group: int, cycles: int,

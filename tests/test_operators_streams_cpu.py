@@ -59,6 +59,7 @@ class World:
         monkeypatch.setattr(torch, "empty", new)
         monkeypatch.setattr(sa, "_raw_stream", None)
         monkeypatch.setattr(sa, "_dev", lambda t, *a, **kw: t.data_ptr())
+        monkeypatch.setattr(sa, "_here", lambda: None)
         for name in self.LIBRARY:
             monkeypatch.setattr(sa.lib, name, call)
 
