@@ -686,13 +686,15 @@ def shiftadd_moe(x: torch.Tensor, logits: torch.Tensor, k: int, gate, up, down, 
                  stream=None) -> torch.Tensor:
     """A gated mixture-of-experts block, ``residual + sum_j w_j D_e(silu(G_e x) * U_e x)`` over
     each token's ``k`` experts, as a new fp16 ``[tokens][K]`` tensor.  ``gate``, ``up`` (N x K
-    layers) and ``down`` (K x N) are ``(packed_bits, exps, q)`` of all experts; ``logits`` fp32
-    ``[tokens][experts]``."""
+    layers) and ``down`` (K x N) are ``(packed_bits, exps, q)`` of all experts; ``x`` fp16
+    ``[tokens][K]``, ``logits`` fp32 ``[tokens][experts]``."""
     other = _other(stream)
     if other is not None:
         return _run_on(other, shiftadd_moe, x, logits, k, gate, up, down, N, K, group, residual,
                        normalize)
     tokens, experts = logits.shape
+    if x.numel() != tokens * K:   # (slots without a row of x would be summed unwritten)
+        raise ValueError(f"x must have {tokens * K} elements, got {x.numel()}")
     slots = tokens * k
     _, weights, offsets, row_of, slot_of = route_experts(logits, k, normalize, stream)
     new = lambda n: torch.empty((slots, n), dtype=torch.float16, device=x.device)  # noqa: E731

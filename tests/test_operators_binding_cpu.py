@@ -125,3 +125,14 @@ def test_host_tensors_are_refused(calls, operator):
             with pytest.raises(ValueError, match=f"{name} must be on the GPU"):
                 f(**{**kw, name: t.as_subclass(torch.Tensor).clone()})
     assert calls == []
+
+
+def test_moe_refuses_activations_that_do_not_match_the_logits(calls):
+    """With fewer rows of x than of logits some slots had no row, and their outputs were summed
+    as they were found in memory."""
+    layer = (*layers(E), 1)
+    down = (on(torch.zeros(E * N_ * K_ // 8, dtype=torch.uint8)), None, 1)
+    for rows in (T - 1, T + 1, 0):
+        with pytest.raises(ValueError, match="x must have"):
+            sa.shiftadd_moe(half(rows, K_), floats(T, E), 2, layer, layer, down, N_, K_, 128)
+    assert calls == []
