@@ -47,12 +47,18 @@ void run_few(const Layer& a, hipStream_t s) {
     else sa_panel::launch(a, s);
 }
 
+// Experts of a few rows and the others by kernels of their own, up to a mean of kFewMean rows.
+// Measured (us, that kernel first, the panel kernel alone second; the rows spread evenly over
+// the experts, and falling with the expert's rank): 8 experts 11008x4096 q=3 mean 2 60 and 87,
+// 52 and 68; mean 4 60 and 82, 69 and 82; mean 5 99 and 82, 76 and 81; mean 8 104 and 82, 90
+// and 82.  16 experts 4096x11008 q=2 mean 2 79 and 104, 81 and 75; mean 4 91 and 105, 115 and
+// 104; mean 8 160 and 111, 142 and 122.  128 experts 768x2048 q=2 mean 4 43 and 52, 47 and 44.
+// Small layers lose by it: 8 experts 1024x1024 q=3 mean 2 11.4 and 10.0, 15.4 and 10.2.
+constexpr int kFewMean = 4;
+
 int run(Layer& a, hipStream_t s) {
     if (a.offsets) {
-        // Experts of a few rows and the others by kernels of their own, where many have few:
-        // 8 slots of 8 experts 39 us against 71 of the panel kernel alone, but 384 slots of 16
-        // experts 174 against 135, since the second kernel waits for the first.
-        if (a.rows <= sa_mx::kExpertRows * a.experts && sa_mx::launch_experts(a, s))
+        if (a.rows <= kFewMean * a.experts && sa_mx::launch_experts(a, s))
             a.few = sa_mx::kExpertRows;
         if (a.rows > a.few) sa_panel::launch(a, s);
     } else if (a.rows == 1 && a.G % 128 == 0) {
