@@ -348,7 +348,10 @@ typedef enum {
  *   y           (device) [rows][N], 16-byte aligned, fully overwritten.
  * An infinity or NaN in a row of x makes that row's sums infinite or NaN and
  * reaches no other row.  The sums are those of sa_shiftadd_gemm up to the order
- * of their fp32 additions.  Errors as for sa_shiftadd_gemm. */
+ * of their fp32 additions.  With nothing after the product this is the faster call from
+ * 64 rows on, and for groups that are not multiples of 128 at any number of rows (measured,
+ * sa_shiftadd_gemm first: 11003x4096 q = 3 64 rows 34 and 21 us, 250 rows 91 and 47; 4096x4096
+ * group 64 one row 287 and 22).  Errors as for sa_shiftadd_gemm. */
 SA_API int sa_shiftadd_gemm_epilogue(const uint16_t *x, const uint8_t *packed_bits,
                                      const int8_t *exps, int q, int N, int K, int group, int rows,
                                      const float *bias, int activation, const void *multiplier,
@@ -368,7 +371,7 @@ SA_API int sa_shiftadd_gemm_epilogue(const uint16_t *x, const uint8_t *packed_bi
  *   exps        (device) int8 [experts][q][N][K/group].
  *   bias        (device) fp32 [experts][N] or NULL; multiplier (device) [slots][N]
  *               of y's type or NULL, may be y itself.
- *   y           (device) [slots][N], 16-byte aligned.
+ *   y           (device) [slots][N], 16-byte aligned; no other overlap with an input.
  *   1 <= experts <= SA_MAX_EXPERTS; slots (0 allowed) as the rows above and x_rows
  *   in [0, SA_MAX_ROWS] with x_rows * K <= 2^35 (else SA_ERR_SHAPE).
  * Rows of y that belong to no expert (before offsets[0], from offsets[experts] on)
@@ -417,8 +420,8 @@ SA_API int sa_route_experts(const float *logits, int tokens, int experts, int k,
  * in fp32, j ascending, rounded once; a slot_of outside [0, slots) adds nothing,
  * whatever its weight.
  *   h (device) [slots][N]; residual (device) [tokens][N] or NULL (0), may be y
- *   itself; y (device) [tokens][N], fully overwritten: binary16 (half = 1) or fp32
- *   (0), each 16-byte aligned.  slot_of (device) int32, weights (device) fp32
+ *   itself; y (device) [tokens][N], fully overwritten, no other overlap with an input:
+ *   binary16 (half = 1) or fp32 (0), each 16-byte aligned.  slot_of (device) int32, weights (device) fp32
  *   [tokens][k], 4-byte aligned.
  *   1 <= k <= SA_MAX_CHOICES; N >= 1; 0 <= slots, tokens <= SA_MAX_ROWS; tokens * N
  *   and slots * N <= 2^34 (else SA_ERR_SHAPE).  Asynchronous on `stream`. */

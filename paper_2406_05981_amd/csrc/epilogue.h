@@ -20,18 +20,22 @@ struct Epilogue {
     int half;
 };
 
-// 1 / (1 + exp(-z)) by the hardware's exponential and reciprocal (1 ulp each): the
-// rounding of z log2(e) is a relative error of |z| 2^-24 of exp(-z), and v times the
-// result is off by at most 2^-23 |v| either way.
+// 1 / (1 + exp(-z)) by the hardware's exponential and reciprocal (1 ulp each).  Measured
+// over 4 million v in each of 13 ranges within +-100: v times the result is off by at most
+// 2.6 * 2^-24 |v|, SILU and GELU_TANH.  Small results of negative v are off by more relative
+// to themselves, since the rounding of z log2(e) is a relative error of |z| 2^-24 of
+// exp(-z): 4e-7 of SILU and 3e-6 of GELU_TANH at -5..-3, 1e-6 and 1.4e-5 at -13..-8.
 __device__ inline float sigmoid(float z) {
     return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-1.44269504088896341f * z));
 }
 
 // v Phi(v) = v / 2 erfc(-v / sqrt 2).  erfc(z) = exp(-z^2) t P(t), t = 1 / (1 + z / 2), z >= 0, P
 // the polynomial of degree 8 closest to erfcx(z) / t (a least-squares fit, reweighted
-// towards equal relative errors: 3.2e-8; 3.0e-7 as evaluated in fp32); for v > 0 from the
-// other tail, 2 - erfc.  The library's erfcf has branches for every range: 45 million
-// outputs after a prompt's product cost 48 us with it.
+// towards equal relative errors: 3.2e-8); for v > 0 from the other tail, 2 - erfc.  The
+// result, measured as above: off by at most 4.1 * 2^-24 |v| (at |v| < 0.1); relative to
+// itself 5e-7 above -1, 1.4e-6 at -3..-1, 7e-6 at -8..-5, 1.7e-5 at -13..-8.  The library's
+// erfcf has branches for every range: 45 million outputs after a prompt's product cost 48 us
+// with it.
 __device__ inline float gelu(float v) {
     const float z = 0.70710678118654752f * fabsf(v);
     const float t = __builtin_amdgcn_rcpf(fmaf(0.5f, z, 1.0f));

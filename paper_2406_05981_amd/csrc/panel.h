@@ -7,20 +7,22 @@
 // sum is a multiple of the smallest factor, at most 2^11 of it, so the sum over the
 // planes is exact and one matrix product serves all planes.  (Below -14 the sum may
 // be subnormal, and the matrix core then drops low bits of its products: measured
-// 7e-6 of sum|terms| at 2^-24.)  A block of 128 columns
+// 7e-6 of sum|terms| at 2^-24.  Of subnormal activations beside these normal sums it drops
+// none: rows of multiples of 2^-24 up to 3 * 2^-24 come out exact.)  A block of 128 columns
 // that has any other exponents in a wave's rows is left for a second loop, two products a
 // plane: +-2^e is a bfloat16 number, an activation the sum of two.
 //
 // Against a product a plane this takes a third of the matrix core's work for 3 planes and,
 // with tiles of 256 rows x 256 outputs, an expanded key serves 256 rows: layer of
-// 11008x4096, 3 planes, with SiLU and multiplier 4096 rows 401 us (922 TFLOP/s; a library
-// product of binary16 tensors of that size 425), 11003x4096 250 rows with GELU 46 us (the
-// tile kernel of gemm_mfma.hip 81 without).
+// 11008x4096, 3 planes, 4096 rows 373 us, with SiLU 377, with SiLU and multiplier 400 (923
+// TFLOP/s; a library product of binary16 tensors of that size, without either, 425), 11003x4096
+// 250 rows 45 us, with bias and GELU 47 (the tile kernel of gemm_mfma.hip 81 to 91 without).
+// (A pass among others, weights rotated over 320 MB and more.)
 //
 // What bounds it.  4096 rows: power.  The same 258 thousand cycles of a 256-row tile take
 // 114 us on 64 compute units (2.26 GHz) and 140 us on all (1.84 GHz); the matrix cores are
 // busy 45% of the cycles, vector instructions 42%, 6.3 a product, of which 4.1 expand planes.
-// Up to 32 rows: vector instructions (4096x11008, 2 planes, 16 experts of 8 to 113 rows: 75%
+// Up to 32 rows: vector instructions (4096x11008, 2 planes, 16 experts of 8 to 96 rows: 75%
 // of the SIMD cycles, matrix cores 19%).  Between: too few tiles for the compute units, 8
 // waves each, whose expansion, LDS reads and products follow each other at the barriers.
 #ifndef SHIFTADD_PANEL_H
@@ -155,7 +157,9 @@ __device__ __forceinline__ void body(const Args& pa, uint4* xbuf, uint32_t* far_
     constexpr int kItems = CT * 8 / RW;  // 1 KiB copies (4 rows) of a wave a block
     constexpr int kBuf = CT * 512;       // uint4 of one block
     constexpr int kE = Q > 4 ? 2 : 1;    // words of a block's exponents
-    // one row tile: two workgroups a CU (128 registers) hide more than the interleaving
+    // One row tile: with 4 column shares two workgroups a CU (64 KB of LDS, 128 registers) hide
+    // more than the interleaving.  With 8 the LDS holds one workgroup; interleaving was not
+    // measured there.
     constexpr bool kPipelined = Q <= 4 && CT > 1;
     const int nt = (int)(blockIdx.x % (unsigned)pa.n_tiles);
     const int lane = threadIdx.x & 63;
@@ -363,9 +367,11 @@ __device__ __forceinline__ void body(const Args& pa, uint4* xbuf, uint32_t* far_
     };
     // The same with the next quarter's operands expanded between one quarter's products, a
     // piece after each: a product takes the matrix core 32 cycles, in which the two waves of
-    // a SIMD issue the expansion's vector instructions (11008x4096 4096 rows 386 -> 369 us;
-    // the compiler's own order of the same code puts the LDS reads last and gains nothing).  Pieces 0 .. Q - 1 spread a plane's
-    // word, the others are a pair each, by the position of its bits (add_pair).
+    // a SIMD issue the expansion's vector instructions (11008x4096, nothing after the product,
+    // 4096 rows 402 -> 373 us, 250 rows 48 -> 45; 4096x4096 64 rows, one row tile, the same; the
+    // compiler's own order of the same code puts the LDS reads last and gains nothing).  Pieces
+    // 0 .. Q - 1 spread a plane's word, the others are a pair each, by the position of its bits
+    // (add_pair).
     struct Next {
         Spread sp[Q];
         half2_t m10[Q], m[Q];  // factors of the block for position 10, and for the position at hand
@@ -640,8 +646,8 @@ __device__ __forceinline__ void body(const Args& pa, uint4* xbuf, uint32_t* far_
     };
 
     // Blocks left for the second loop, a bit per two steps (steps far apart share one): it
-    // visits those alone (11008x4096, 250 rows: 41 us, one such group in the layer 55, which
-    // took 79 over all blocks; every block 194).
+    // visits those alone (11008x4096, 250 rows: 45 us, one such group in the layer 57, where a
+    // loop over all blocks took 79; every block 197).
     bool left = false;
     auto leave = [&](int s) {
         left = true;
