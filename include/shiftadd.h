@@ -348,11 +348,12 @@ typedef enum {
  *   y           (device) [rows][N], 16-byte aligned, fully overwritten.
  * An infinity or NaN in a row of x makes that row's sums infinite or NaN and
  * reaches no other row.  The sums are those of sa_shiftadd_gemm up to the order
- * of their fp32 additions.  (A factor multiplies sums of at most 128 columns:
- * above 2^100 a longer group whose parts cancel may leave fp32 before they meet.)  With nothing after the product this is the faster call from
- * 64 rows on, and for groups that are not multiples of 128 at any number of rows (measured,
- * sa_shiftadd_gemm first: 11003x4096 q = 3 64 rows 34 and 21 us, 250 rows 91 and 47; 4096x4096
- * group 64 one row 287 and 22).  Errors as for sa_shiftadd_gemm. */
+ * of their fp32 additions.  (A factor multiplies sums of at most 128 columns: above
+ * 2^100 a longer group whose parts cancel may leave fp32 before they meet.)  With
+ * nothing after the product this is the faster call from 64 rows on, and for groups
+ * that are not multiples of 128 at any number of rows (measured, sa_shiftadd_gemm
+ * first: 11003x4096 q = 3 64 rows 34 and 21 us, 250 rows 91 and 47; 4096x4096 group
+ * 64 one row 287 and 22).  Errors as for sa_shiftadd_gemm. */
 SA_API int sa_shiftadd_gemm_epilogue(const uint16_t *x, const uint8_t *packed_bits,
                                      const int8_t *exps, int q, int N, int K, int group, int rows,
                                      const float *bias, int activation, const void *multiplier,
